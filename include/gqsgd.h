@@ -313,6 +313,111 @@ gq_status gq_sparse_aggregate(const uint32_t *const *indices /* host */, const i
                               const uint32_t *const *tile_starts /* host */, int K, int64_t d,
                               const gq_params *p /* host */, void *agg_out, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The layers around the gradient exchange: dropout from the generator above, root-mean-square norm with the residual's
+ * addition, 4-bit weights under group scales and their product with rows of activations.
+ *
+ * Matrices are dense and row-major; their first element is 16-byte aligned, their rows need not be (any row length).
+ * Every call is defined for 0 rows and 0 columns (nothing is written but the sums that are empty).  Sums, norms and scales
+ * are formed in binary32 or wider and a result is rounded once, to nearest even, to the type that it is stored in.
+ * Sizes that one launch cannot cover (about 2^35 elements) are answered with GQ_ERR_INVALID_ARG.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef enum {
+    GQ_F32 = 0,    /* binary32                                              */
+    GQ_BF16 = 1,   /* bfloat16                                              */
+    GQ_F16 = 2,    /* binary16                                              */
+    GQ_I8 = 3,     /* int8 codes -127 .. 127 under a scale                  */
+    GQ_E4M3 = 4    /* 8-bit floats (OCP e4m3, no infinities) under a scale  */
+} gq_dtype;
+
+/* Dropout: element (r, c) of a matrix of n columns has the index g = index_base + 8 ceil(n/8) r + c in the random stream and
+ * draws rng_bits bits from Philox4x32-10 with key (lo32(seed), hi32(seed)):
+ *   32 bits   word g mod 4 of the call with counter (lo32(g/4), hi32(g/4), worker, 3)
+ *   16 bits   the low (g even) or high (g odd) half of word (g mod 8) / 2 of the call with counter (lo32(g/8), hi32(g/8), worker, 3)
+ * With t = min(rne(p 2^rng_bits), 2^rng_bits - 1) it is dropped (becomes 0, whatever it held) iff its draw is below t, and
+ * otherwise multiplied by fl32(2^rng_bits / (2^rng_bits - t)), which keeps the mean exactly.  No mask is stored: the backward
+ * pass draws the same bits again.  (The other draws of this library have 0, 1 or 2 in the fourth counter word.)
+ * A matrix cut between rows gives the same bits as the whole when each part passes its offset, 8 ceil(n/8) times its first row. */
+typedef struct {
+    double p;            /* probability of being dropped, 0 <= p < 1                                              */
+    uint64_t seed;       /* Philox key                                                                            */
+    int64_t index_base;  /* index of element (0, 0), >= 0 and a multiple of 4 (of 8 with rng_bits = 16)           */
+    uint32_t worker;     /* distinct workers (layers, ranks) draw independently                                   */
+    int32_t rng_bits;    /* 32 (0 reads as 32) or 16                                                              */
+} gq_dropout_params;
+
+/* out = residual + dropout(x), or dropout(x) without a residual; one rounding to `dtype`.  The backward pass is the same call on
+ * the gradient without a residual (the residual's gradient is the incoming one).
+ *   x, residual, out  device [rows][n] of GQ_F32, GQ_BF16 or GQ_F16; residual may be NULL; out may be x or residual */
+gq_status gq_dropout(const void *x, const void *residual, int64_t rows, int64_t n, gq_dtype dtype,
+                     const gq_dropout_params *drop /* host */, void *out, void *hip_stream);
+
+/* Root-mean-square norm of each row with the residual's addition in front of it:
+ *   h = residual + dropout(x);  rstd = fl32(1 / sqrt(sum(h^2) / n + eps)) from a binary64 sum;  y = (h rstd) weight
+ * h is kept in binary32 within the call; sum_out is its rounded copy, out is formed from the unrounded one.
+ *   x, residual    device [rows][n] of `dtype` (GQ_F32, GQ_BF16, GQ_F16); residual may be NULL; n <= GQ_RMS_NORM_MAX_N
+ *   weight         device [n] of weight_dtype: GQ_F32 or `dtype`
+ *   eps            > 0 and finite
+ *   drop           NULL: no dropout
+ *   sum_out        device [rows][n] of `dtype`: h, or NULL; may be x or residual
+ *   out            device [rows][n] of out_dtype; may be x or residual where out_dtype is `dtype`, not sum_out
+ *   out_dtype      `dtype`, or GQ_I8 / GQ_E4M3: 8 bits under a scale per row.  With a = max |y| of the row and top = 127 or 448,
+ *                  scale = fl32(a / top) and the code is y fl32(1 / scale) rounded to nearest even.  A row of zeros, and one
+ *                  whose 1 / scale is not finite, has scale 0 and codes 0; a row that is not finite has scale NaN and codes 0.
+ *   scales_out     device fp32[rows] for the 8-bit types, else NULL
+ *   rstd_out       device fp32[rows], or NULL: what the backward pass takes */
+#define GQ_RMS_NORM_MAX_N 32768
+gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t n, gq_dtype dtype, const void *weight,
+                      gq_dtype weight_dtype, float eps, const gq_dropout_params *drop /* host, or NULL */, void *sum_out,
+                      void *out, gq_dtype out_dtype, float *scales_out, float *rstd_out, void *hip_stream);
+
+/* The backward pass of gq_rms_norm (outputs in `dtype`).  With xh = h rstd and g = dy weight:
+ *   dh = dsum + rstd (g - xh mean(g xh)) (the mean from a binary64 sum);  dweight = sum over the rows of dy xh
+ *   dy, h, rstd   the gradient of out, and sum_out (x itself where there was no residual and no dropout) and rstd_out of the call
+ *   dsum          the gradient that reaches h past the norm (the residual stream's), or NULL
+ *   drop          the forward call's, or NULL
+ *   dres_out      device [rows][n]: dh, the residual's gradient; only with drop (else GQ_ERR_INVALID_ARG), or NULL; may be dsum
+ *   dx_out        device [rows][n]: x's gradient: dh, with drop after dropout; may be dy or dsum, not dres_out
+ *   dweight_out   device fp32[n], overwritten, or NULL.  Its bits do not depend on scheduling (no atomics).
+ *   workspace     device scratch of at least gq_rms_norm_workspace_bytes(rows, n) bytes, 16-byte aligned, where dweight_out is
+ *                 given; overwritten; not to be shared by calls that may run concurrently */
+size_t gq_rms_norm_workspace_bytes(int64_t rows, int64_t n);
+gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, int64_t rows, int64_t n, gq_dtype dtype,
+                               const void *weight, gq_dtype weight_dtype, const float *rstd,
+                               const gq_dropout_params *drop /* host, or NULL */, void *dres_out, void *dx_out,
+                               float *dweight_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* 4-bit weights under group scales.  A matrix [rows][cols] is stored as codes -7 .. 7 of the linear grid (s = 7) in the
+ * nibbles of GQ_PACK_I4, every row padded with zero codes to gq_w4_row_bytes(cols) = 16 ceil(cols/32) bytes, and one scale for
+ * each `group` consecutive columns of a row (the last group may be short): scales [rows][ceil(cols/group)] of GQ_F32 or
+ * GQ_BF16.  group is 32, 64 or 128.  Column c of a row stands for code times the scale of group c / group.
+ *
+ * gq_group_quantize: with a = max |w| of the group, scale = fl32(a / 7) rounded to scale_dtype; the code is w / scale rounded to
+ * nearest, ties to even (the exact quotient), -7 .. 7.  A group of zeros, and one whose 1 / scale is not finite in binary32, has
+ * scale 0 and codes 0; a group that is not finite has scale NaN and codes 0.
+ *   w           device [rows][cols] of `dtype` (GQ_F32, GQ_BF16, GQ_F16)
+ *   codes_out   device [rows][gq_w4_row_bytes(cols)] bytes; scales_out device [rows][ceil(cols/group)] */
+int64_t gq_w4_row_bytes(int64_t cols);          /* 0 if cols is out of range */
+gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype dtype, int group, void *codes_out,
+                            void *scales_out, gq_dtype scale_dtype, void *hip_stream);
+
+/* The values that the codes stand for: out = code * scale, device [rows][cols] of `dtype`.  (A nibble of -8 stands for -8.) */
+gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype scale_dtype, int64_t rows, int64_t cols, int group,
+                              void *out, gq_dtype dtype, void *hip_stream);
+
+/* Rows of activations times 4-bit weights: y[i][r] = x_scales[i] * sum over groups g of scale[r][g] * (sum over c in g of
+ * code[r][c] x[i][c]) + bias[r].  Meant for few rows (m from 1 to some tens, the weights are read once for 64 of them); any m works.
+ *   x         device [m][cols] of x_dtype: GQ_BF16, GQ_F16, or GQ_I8 (codes, as gq_rms_norm writes them)
+ *   x_scales  device fp32[m] with GQ_I8, else NULL
+ *   bias      device [rows] of y_dtype, or NULL
+ *   y         device [m][rows] of y_dtype: GQ_F32, GQ_BF16 or GQ_F16
+ * Products of int8 activations are summed exactly within a group.  Sums of GQ_BF16 and GQ_F16 activations are formed with the
+ * codes moved by 24 (matrix instructions take 24 + code) and corrected by 24 times the sum of x: in binary32, so exact to a few
+ * 2^-24 of 24 sum |x| over up to 128 columns.  A row of x that holds an infinity or a NaN gives NaN. */
+gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t m, gq_dtype x_dtype, const void *codes, const void *scales,
+                       gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, const void *bias, void *y, gq_dtype y_dtype,
+                       void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,18 +21,26 @@ GQ_LINEAR, GQ_EXP = 0, 1
 GQ_PACK_I8, GQ_PACK_I4, GQ_PACK_U8_SIGNPLANE, GQ_PACK_U4_SIGNPLANE = 0, 1, 2, 3
 GQ_AGG_I32, GQ_AGG_I16 = 0, 1
 GQ_FLAG_WRITE_WINDOWS_OFF, GQ_FLAG_WRITE_WINDOWS_ON = 1, 2
+GQ_F32, GQ_BF16, GQ_F16, GQ_I8, GQ_E4M3 = 0, 1, 2, 3, 4
+GQ_RMS_NORM_MAX_N = 32768
 
 # every symbol include/gqsgd.h declares
 EXPORTS = ("gq_version", "gq_status_string", "gq_check_width", "gq_sparse_nnz_bound", "gq_norm_workspace_bytes", "gq_global_norm",
            "gq_global_norm_static", "gq_bucketed_workspace_bytes", "gq_bucketed_quantize_aggregate",
            "gq_quantize", "gq_int_aggregate", "gq_dequantize", "gq_fused_quantize_aggregate", "gq_exp_reduce", "gq_avg_reduce", "gq_compact_workspace_bytes", "gq_tile_starts_len", "gq_compact",
            "gq_quantize_compact",
-           "gq_sparse_aggregate")
+           "gq_sparse_aggregate",
+           "gq_dropout", "gq_rms_norm", "gq_rms_norm_workspace_bytes", "gq_rms_norm_backward",
+           "gq_w4_row_bytes", "gq_group_quantize", "gq_group_dequantize", "gq_w4_matvec")
 
 
 class gq_params(C.Structure):
     _fields_ = [("scheme", C.c_int32), ("s", C.c_int32), ("pack", C.c_int32), ("agg", C.c_int32),
                 ("rng_bits", C.c_int32), ("flags", C.c_int32), ("seed", C.c_uint64)]
+
+
+class gq_dropout_params(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("index_base", C.c_int64), ("worker", C.c_uint32), ("rng_bits", C.c_int32)]
 
 
 class GQError(RuntimeError):
@@ -50,6 +58,7 @@ def _load():
     lib = C.CDLL(LIB_PATH)
     vp, i64, u32, i32, sz = C.c_void_p, C.c_int64, C.c_uint32, C.c_int, C.c_size_t
     pp = C.POINTER(gq_params)
+    dp, f32 = C.POINTER(gq_dropout_params), C.c_float
     sigs = {
         "gq_version": (C.c_int, []),
         "gq_status_string": (C.c_char_p, [i32]),
@@ -72,6 +81,14 @@ def _load():
         "gq_sparse_aggregate": (i32, [C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(i64), C.POINTER(vp), i32, i64, pp, vp, vp]),
         "gq_fused_quantize_aggregate": (i32, [C.POINTER(vp), i32, i64, vp, pp, i64, vp, vp, C.POINTER(vp),
                                                C.POINTER(vp), vp]),
+        "gq_dropout": (i32, [vp, vp, i64, i64, i32, dp, vp, vp]),
+        "gq_rms_norm": (i32, [vp, vp, i64, i64, i32, vp, i32, f32, dp, vp, vp, i32, vp, vp, vp]),
+        "gq_rms_norm_workspace_bytes": (sz, [i64, i64]),
+        "gq_rms_norm_backward": (i32, [vp, vp, vp, i64, i64, i32, vp, i32, vp, dp, vp, vp, vp, vp, sz, vp]),
+        "gq_w4_row_bytes": (i64, [i64]),
+        "gq_group_quantize": (i32, [vp, i64, i64, i32, i32, vp, vp, i32, vp]),
+        "gq_group_dequantize": (i32, [vp, vp, i32, i64, i64, i32, vp, i32, vp]),
+        "gq_w4_matvec": (i32, [vp, vp, i64, i32, vp, vp, i32, i64, i64, i32, vp, vp, i32, vp]),
     }
     for name, (res, args) in sigs.items():
         f = getattr(lib, name)
@@ -242,3 +259,66 @@ def quantize_compact(x, norm, params, worker, index_base, indices_out, values_ou
 
 def sparse_aggregate(indices, values, counts, d, params, agg_out, stream=None, tile_starts=None):
     _check(_m.sparse_aggregate(indices, values, counts, int(d), params, agg_out, tile_starts, _stream(stream)), "gq_sparse_aggregate")
+
+
+def make_dropout(p, seed, worker=0, index_base=0, rng_bits=32):
+    """The parameters of a dropout: probability, Philox key, worker word, index of the first element, random bits per element."""
+    return gq_dropout_params(float(p), int(seed), int(index_base), int(worker), int(rng_bits))
+
+
+def _drop(drop):
+    if drop is not None and not isinstance(drop, gq_dropout_params):
+        raise TypeError("drop must come from make_dropout")
+    return drop
+
+
+def dropout(x, drop, out, residual=None, stream=None):
+    """gq_dropout: out = residual + dropout(x) over the last dimension's rows.  The backward pass is the same call on the gradient."""
+    _check(_m.dropout(x, _drop(drop), out, residual, _stream(stream)), "gq_dropout")
+
+
+def rms_norm(x, weight, eps, out, residual=None, sum_out=None, scales_out=None, rstd_out=None, drop=None, stream=None):
+    """gq_rms_norm: h = residual + dropout(x) into sum_out, h / rms(h) * weight into out; an int8 or float8_e4m3fn out takes codes
+    and scales_out their scales, one a row."""
+    _check(_m.rms_norm(x, weight, eps, out, residual, sum_out, scales_out, rstd_out, _drop(drop), _stream(stream)), "gq_rms_norm")
+
+
+def rms_norm_workspace_bytes(rows, n):
+    return int(_lib.gq_rms_norm_workspace_bytes(int(rows), int(n)))
+
+
+def rms_norm_backward(dy, h, weight, rstd, dx_out, dsum=None, dres_out=None, dweight_out=None, drop=None, workspace=None, stream=None):
+    """gq_rms_norm_backward: the gradients of x, of the residual (dres_out, with drop only; else it is dx_out) and of the weight.
+    Returns the workspace used (None without dweight_out)."""
+    if workspace is None and dweight_out is not None:
+        n = dy.size(-1)
+        nbytes = max(rms_norm_workspace_bytes(dy.numel() // n if n else 0, n), 16)
+        if stream is None:
+            workspace = _workspace(nbytes, dy)
+        else:                                              # memory of that stream's own, so that it may be let go of at once
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+                workspace = _workspace(nbytes, dy)
+    _check(_m.rms_norm_backward(dy, h, weight, rstd, dx_out, dsum, dres_out, dweight_out, _drop(drop), workspace, _stream(stream)),
+           "gq_rms_norm_backward")
+    return workspace
+
+
+def w4_row_bytes(cols):
+    return int(_lib.gq_w4_row_bytes(int(cols)))
+
+
+def group_quantize(w, group, codes_out, scales_out, stream=None):
+    """gq_group_quantize: w [rows, cols] to 4-bit codes (uint8 [rows, w4_row_bytes(cols)]) under a scale (float32 or bfloat16) for
+    every `group` columns of a row."""
+    _check(_m.group_quantize(w, int(group), codes_out, scales_out, _stream(stream)), "gq_group_quantize")
+
+
+def group_dequantize(codes, scales, group, out, stream=None):
+    """gq_group_dequantize: the values that the codes stand for, into out [rows, cols]."""
+    _check(_m.group_dequantize(codes, scales, int(group), out, _stream(stream)), "gq_group_dequantize")
+
+
+def w4_matvec(x, codes, scales, group, out, x_scales=None, bias=None, stream=None):
+    """gq_w4_matvec: out [..., rows] = x [..., cols] times the transposed 4-bit weights, plus bias; x bfloat16, float16, or int8
+    codes under x_scales, one a row."""
+    _check(_m.w4_matvec(x, codes, scales, int(group), out, x_scales, bias, _stream(stream)), "gq_w4_matvec")

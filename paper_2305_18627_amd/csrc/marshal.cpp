@@ -21,7 +21,9 @@ namespace {
 #define GQ_ENTRY_POINTS(X)                                                                                              \
     X(gq_global_norm) X(gq_global_norm_static) X(gq_quantize) X(gq_int_aggregate) X(gq_dequantize)                      \
     X(gq_fused_quantize_aggregate) X(gq_bucketed_quantize_aggregate) X(gq_exp_reduce) X(gq_avg_reduce) X(gq_compact)     \
-    X(gq_quantize_compact) X(gq_sparse_aggregate) X(gq_tile_starts_len)
+    X(gq_quantize_compact) X(gq_sparse_aggregate) X(gq_tile_starts_len) X(gq_dropout) X(gq_rms_norm)                     \
+    X(gq_rms_norm_backward) X(gq_rms_norm_workspace_bytes) X(gq_w4_row_bytes) X(gq_group_quantize) X(gq_group_dequantize) \
+    X(gq_w4_matvec)
 struct Library {
 #define GQ_FIELD(name) decltype(&name) name##_;
     GQ_ENTRY_POINTS(GQ_FIELD)
@@ -388,6 +390,215 @@ PyObject *sparse_aggregate(PyObject *const *a)
     });
 }
 
+// ---- the layers around the exchange: shapes and types are the tensors' own ----------------------------------------
+
+[[noreturn]] void refuse(const char *what)
+{
+    PyErr_SetString(PyExc_ValueError, what);
+    throw Refused();
+}
+
+// a contiguous tensor on the GPU
+const at::Tensor &matrix(PyObject *o, const char *what)
+{
+    const at::Tensor &t = tensor(o, what);
+    need(t, 0, what);
+    return t;
+}
+// the address of a matrix of n elements, and of no others; None: a null address
+void *sized(PyObject *o, int64_t n, at::ScalarType type, const char *what)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = matrix(o, what);
+    if (t.numel() != n || t.scalar_type() != type) {
+        PyErr_Format(PyExc_ValueError, "%s must hold %lld elements of %s", what, (long long)n, c10::toString(type));
+        throw Refused();
+    }
+    return t.data_ptr();
+}
+void *given(PyObject *o, int64_t n, at::ScalarType type, const char *what)
+{
+    if (o != Py_None) return sized(o, n, type, what);
+    PyErr_Format(PyExc_TypeError, "%s must be a tensor", what);
+    throw Refused();
+}
+
+gq_dtype dtype_of(const at::Tensor &t, const char *what)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: return GQ_F32;
+    case at::kBFloat16: return GQ_BF16;
+    case at::kHalf: return GQ_F16;
+    case at::kChar: return GQ_I8;
+    case at::kFloat8_e4m3fn: return GQ_E4M3;
+    default: break;
+    }
+    PyErr_Format(PyExc_ValueError, "%s has a type that the call does not take: %s", what, c10::toString(t.scalar_type()));
+    throw Refused();
+}
+
+// rows and columns of a tensor [..., n]
+struct Shape {
+    int64_t rows = 1, n;
+    Shape(const at::Tensor &t, const char *what)
+    {
+        if (t.dim() < 1) {
+            PyErr_Format(PyExc_ValueError, "%s must have at least one dimension", what);
+            throw Refused();
+        }
+        n = t.size(-1);
+        for (int64_t i = 0; i + 1 < t.dim(); i++) rows *= t.size(i);
+    }
+    int64_t numel() const { return rows * n; }
+};
+
+// the stream of a call, whose tensors must all be on the current device (a stream belongs to one, and so does a launch)
+void *stream_for(PyObject *o, std::initializer_list<PyObject *> tensors)
+{
+    PyObject *dev = PyObject_CallObject(current_device, nullptr);
+    if (!dev) throw Refused();
+    const int64_t now = PyLong_AsLongLong(dev);
+    Py_DECREF(dev);
+    if (now == -1 && PyErr_Occurred()) throw Refused();
+    for (PyObject *t : tensors)
+        if (t != Py_None && THPVariable_Unpack(t).device().index() != now) refuse("every tensor must be on the current device");
+    return stream_of(o);
+}
+
+struct DropParams {                                                    // a ctypes gq_dropout_params, or None
+    Py_buffer view;
+    bool there;
+    explicit DropParams(PyObject *o) : there(o != Py_None)
+    {
+        if (!there) return;
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Refused();
+        if (view.len != (Py_ssize_t)sizeof(gq_dropout_params)) {
+            PyBuffer_Release(&view);
+            there = false;
+            PyErr_SetString(PyExc_TypeError, "drop must be a gq_dropout_params");
+            throw Refused();
+        }
+    }
+    ~DropParams() { if (there) PyBuffer_Release(&view); }
+    DropParams(const DropParams &) = delete;
+    DropParams &operator=(const DropParams &) = delete;
+    const gq_dropout_params *get() const { return there ? reinterpret_cast<const gq_dropout_params *>(view.buf) : nullptr; }
+};
+
+// x, drop, out, residual, stream
+PyObject *dropout(PyObject *const *a)
+{
+    const DropParams p(a[1]);
+    const at::Tensor &x = matrix(a[0], "x");
+    const Shape s(x, "x");
+    const gq_dtype t = dtype_of(x, "x");
+    void *out = given(a[2], s.numel(), x.scalar_type(), "out"), *res = sized(a[3], s.numel(), x.scalar_type(), "residual");
+    void *xp = x.data_ptr(), *st = stream_for(a[4], {a[0], a[2], a[3]});
+    return call([&] { return lib.gq_dropout_(xp, res, s.rows, s.n, t, p.get(), out, st); });
+}
+
+// x, weight, eps, out, residual, sum_out, scales_out, rstd_out, drop, stream
+PyObject *rms_norm(PyObject *const *a)
+{
+    const DropParams p(a[8]);
+    const at::Tensor &x = matrix(a[0], "x"), &w = matrix(a[1], "weight"), &o = matrix(a[3], "out");
+    const Shape s(x, "x");
+    const gq_dtype t = dtype_of(x, "x"), wt = dtype_of(w, "weight"), ot = dtype_of(o, "out");
+    const double eps = PyFloat_AsDouble(a[2]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Refused();
+    if (w.numel() != s.n || o.numel() != s.numel()) refuse("weight or out has another size than x");
+    void *res = sized(a[4], s.numel(), x.scalar_type(), "residual"), *sum = sized(a[5], s.numel(), x.scalar_type(), "sum_out");
+    void *scales = sized(a[6], s.rows, at::kFloat, "scales_out"), *rstd = sized(a[7], s.rows, at::kFloat, "rstd_out");
+    void *xp = x.data_ptr(), *wp = w.data_ptr(), *op = o.data_ptr(), *st = stream_for(a[9], {a[0], a[1], a[3], a[4], a[5], a[6], a[7]});
+    return call([&] {
+        return lib.gq_rms_norm_(xp, res, s.rows, s.n, t, wp, wt, (float)eps, p.get(), sum, op, ot, (float *)scales, (float *)rstd, st);
+    });
+}
+
+// dy, h, weight, rstd, dx_out, dsum, dres_out, dweight_out, drop, workspace, stream
+PyObject *rms_norm_backward(PyObject *const *a)
+{
+    const DropParams p(a[8]);
+    const at::Tensor &dy = matrix(a[0], "dy"), &w = matrix(a[2], "weight");
+    const Shape s(dy, "dy");
+    const gq_dtype t = dtype_of(dy, "dy"), wt = dtype_of(w, "weight");
+    const at::ScalarType type = dy.scalar_type();
+    if (w.numel() != s.n) refuse("weight has another size than a row of dy");
+    void *h = given(a[1], s.numel(), type, "h"), *rstd = given(a[3], s.rows, at::kFloat, "rstd"), *dx = given(a[4], s.numel(), type, "dx_out");
+    void *dsum = sized(a[5], s.numel(), type, "dsum"), *dres = sized(a[6], s.numel(), type, "dres_out");
+    void *dw = sized(a[7], s.n, at::kFloat, "dweight_out"), *ws = nullptr;
+    size_t bytes = 0;
+    if (a[9] != Py_None) {
+        const at::Tensor &u = matrix(a[9], "workspace");
+        ws = u.data_ptr();
+        bytes = (size_t)(u.numel() * (int64_t)u.element_size());
+    }
+    void *yp = dy.data_ptr(), *wp = w.data_ptr(), *st = stream_for(a[10], {a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[9]});
+    return call([&] {
+        return lib.gq_rms_norm_backward_(yp, h, dsum, s.rows, s.n, t, wp, wt, (const float *)rstd, p.get(), dres, dx, (float *)dw, ws, bytes, st);
+    });
+}
+
+// codes [rows][row bytes] and scales [rows][groups] of a matrix [rows][cols]
+struct Weights {
+    void *codes, *scales;
+    int64_t rows, cols;
+    int group;
+    gq_dtype type;
+    Weights(PyObject *codes_, PyObject *scales_, PyObject *group_, int64_t cols_) : cols(cols_)
+    {
+        const at::Tensor &c = matrix(codes_, "codes"), &s = matrix(scales_, "scales");
+        const int64_t g = integer(group_);
+        if (g < 1 || g > (1 << 20)) refuse("group must be 32, 64 or 128");
+        group = (int)g;
+        if (c.scalar_type() != at::kByte || c.dim() != 2 || c.size(1) != lib.gq_w4_row_bytes_(cols)) refuse("codes must be uint8 of rows x w4_row_bytes(columns)");
+        rows = c.size(0);
+        if (s.numel() != rows * ((cols + g - 1) / g)) refuse("scales must hold one scale a group");
+        type = dtype_of(s, "scales");
+        codes = c.data_ptr();
+        scales = s.data_ptr();
+    }
+};
+
+// w, group, codes_out, scales_out, stream
+PyObject *group_quantize(PyObject *const *a)
+{
+    const at::Tensor &w = matrix(a[0], "w");
+    const Shape s(w, "w");
+    const gq_dtype t = dtype_of(w, "w");
+    const Weights out(a[2], a[3], a[1], s.n);
+    if (out.rows != s.rows) refuse("w and codes_out differ in rows");
+    void *wp = w.data_ptr(), *st = stream_for(a[4], {a[0], a[2], a[3]});
+    return call([&] { return lib.gq_group_quantize_(wp, s.rows, s.n, t, out.group, out.codes, out.scales, out.type, st); });
+}
+
+// codes, scales, group, out, stream
+PyObject *group_dequantize(PyObject *const *a)
+{
+    const at::Tensor &o = matrix(a[3], "out");
+    const Shape s(o, "out");
+    const gq_dtype t = dtype_of(o, "out");
+    const Weights in(a[0], a[1], a[2], s.n);
+    if (in.rows != s.rows) refuse("codes and out differ in rows");
+    void *op = o.data_ptr(), *st = stream_for(a[4], {a[0], a[1], a[3]});
+    return call([&] { return lib.gq_group_dequantize_(in.codes, in.scales, in.type, s.rows, s.n, in.group, op, t, st); });
+}
+
+// x, codes, scales, group, out, x_scales, bias, stream
+PyObject *w4_matvec(PyObject *const *a)
+{
+    const at::Tensor &x = matrix(a[0], "x"), &y = matrix(a[4], "out");
+    const Shape s(x, "x"), so(y, "out");
+    const gq_dtype t = dtype_of(x, "x"), yt = dtype_of(y, "out");
+    const Weights w(a[1], a[2], a[3], s.n);
+    if (so.rows != s.rows || so.n != w.rows) refuse("out must be the rows of x by the rows of the weights");
+    void *xs = sized(a[5], s.rows, at::kFloat, "x_scales"), *bias = sized(a[6], w.rows, y.scalar_type(), "bias");
+    void *xp = x.data_ptr(), *yp = y.data_ptr(), *st = stream_for(a[7], {a[0], a[1], a[2], a[4], a[5], a[6]});
+    return call([&] {
+        return lib.gq_w4_matvec_(xp, (const float *)xs, s.rows, t, w.codes, w.scales, w.type, w.rows, s.n, w.group, bias, yp, yt, st);
+    });
+}
+
 // a dict of addresses by name, torch's functions for the current device and a device's current stream
 PyObject *bind(PyObject *const *a)
 {
@@ -426,6 +637,12 @@ PyMethodDef methods[] = {
     GQ_METHOD("compact", 9, compact),
     GQ_METHOD("quantize_compact", 11, quantize_compact),
     GQ_METHOD("sparse_aggregate", 8, sparse_aggregate),
+    GQ_METHOD("dropout", 5, dropout),
+    GQ_METHOD("rms_norm", 10, rms_norm),
+    GQ_METHOD("rms_norm_backward", 11, rms_norm_backward),
+    GQ_METHOD("group_quantize", 5, group_quantize),
+    GQ_METHOD("group_dequantize", 5, group_dequantize),
+    GQ_METHOD("w4_matvec", 8, w4_matvec),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,186 @@
+// 4-bit weights under group scales: making them, unfolding them, and their product with rows of activations.
+// The contract of the entry points is stated in include/gqsgd.h.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+
+#include "gqsgd.h"
+#include "gq_layers.hpp"
+
+namespace gq {
+
+// w / scale to the nearest integer, ties to even, of the exact quotient: the product with fl32(1 / scale) is off by less than
+// 2^-22 and so rounds to the nearest integer or, next to a border, its neighbour.  w - q scale is exact there (it is a multiple of
+// half an ulp of scale and below scale), and says which.
+__device__ __forceinline__ float code_of_quotient(float w, float scale, float inv)
+{
+    float q = __builtin_rintf(w * inv);
+    const float r = __builtin_fmaf(-q, scale, w), twice = 2.0f * __builtin_fabsf(r);
+    const bool odd = (int)q & 1;
+    if (twice > scale || (twice == scale && odd)) q += __builtin_copysignf(1.0f, r);
+    return __builtin_amdgcn_fmed3f(q, -7.0f, 7.0f);
+}
+
+template <typename S> struct GroupScale { S stored; float scale, inv; };
+template <typename S> __device__ __forceinline__ GroupScale<S> group_scale(uint32_t top_bits)
+{
+    if (top_bits >= 0x7F800000u) return {(S)__builtin_nanf(""), 0.0f, 0.0f};
+    const S stored = (S)(__uint_as_float(top_bits) / 7.0f);
+    const float scale = (float)stored, inv = 1.0f / scale;
+    if (!(inv <= 3.402823466e+38f)) return {(S)0.0f, 0.0f, 0.0f};
+    return {stored, scale, inv};
+}
+
+// A lane per group.
+template <typename T, typename S>
+__global__ void __launch_bounds__(kBlock)
+group_quantize_kernel(const T *w, int64_t rows, int64_t cols, int group, int groups, int64_t row_bytes, uint8_t *codes, S *scales)
+{
+    const int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (u >= rows * groups) return;
+    const int64_t row = u / groups, first = (u - row * groups) * group;
+    const T *p = w + row * cols + first;
+    const int valid = (int)(cols - first < group ? cols - first : group);
+    uint32_t m = 0;
+    for (int i = 0; i < valid; i++) m = max(m, __float_as_uint((float)p[i]) & 0x7FFFFFFFu);
+    const GroupScale<S> gs = group_scale<S>(m);
+    scales[u] = gs.stored;
+    uint8_t *out = codes + row * row_bytes + first / 2;
+    const int padded = (valid + 31) / 32 * 32;
+    for (int i = 0; i < padded; i += 2) {
+        uint32_t b = 0;
+        for (int k = 0; k < 2; k++) {
+            if (i + k >= valid || gs.inv == 0.0f) continue;
+            b |= ((uint32_t)(int)code_of_quotient((float)p[i + k], gs.scale, gs.inv) & 15u) << (4 * k);
+        }
+        out[i / 2] = (uint8_t)b;
+    }
+}
+
+// A lane per eight columns.
+template <typename T, typename S>
+__global__ void __launch_bounds__(kBlock)
+group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, int group, int groups, int64_t row_words, T *out)
+{
+    const int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    const int64_t per_row = (cols + 7) / 8;
+    if (u >= rows * per_row) return;
+    const int64_t row = u / per_row, c = (u - row * per_row) * 8;
+    const uint32_t word = codes[row * row_words + c / 8];
+    const float scale = (float)scales[row * groups + c / group];
+    float v[8];
+    for (int i = 0; i < 8; i++) v[i] = (float)((int)(word << (28 - 4 * i)) >> 28) * scale;
+    store8(out + row * cols + c, (int)(cols - c < 8 ? cols - c : 8), v);
+}
+
+// A wave per element of y.
+template <typename X, typename S>
+__global__ void __launch_bounds__(64)
+w4_matvec_kernel(const X *x, const float *x_scales, const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, int group, int groups,
+                 int64_t row_words, const void *bias, void *y, int y_dtype)
+{
+    const int64_t r = blockIdx.x, m = blockIdx.y;
+    double sum = 0.0;
+    for (int64_t c = threadIdx.x * 8; c < cols; c += 64 * 8) {
+        const uint32_t word = codes[r * row_words + c / 8];
+        float s = 0.0f, t = 0.0f;
+        for (int i = 0; i < 8 && c + i < cols; i++) {
+            const float xv = (float)x[m * cols + c + i];
+            s += xv * (float)(24 + ((int)(word << (28 - 4 * i)) >> 28));
+            t += xv;
+        }
+        sum += (double)(s - 24.0f * t) * (double)(float)scales[r * groups + c / group];
+    }
+    float v = (float)wave_sum(sum);
+    if (x_scales) v *= x_scales[m];
+    if (threadIdx.x != 0) return;
+    const int64_t at = m * rows + r;
+    if (y_dtype == GQ_F32) ((float *)y)[at] = v + (bias ? ((const float *)bias)[r] : 0.0f);
+    if (y_dtype == GQ_BF16) ((bf16 *)y)[at] = (bf16)(v + (bias ? (float)((const bf16 *)bias)[r] : 0.0f));
+    if (y_dtype == GQ_F16) ((f16 *)y)[at] = (f16)(v + (bias ? (float)((const f16 *)bias)[r] : 0.0f));
+}
+
+static gq_status check_weights(int64_t rows, int64_t cols, int group, int scale_dtype)
+{
+    if (!matrix_fits(rows, cols) || (group != 32 && group != 64 && group != 128)) return GQ_ERR_INVALID_ARG;
+    return scale_dtype == GQ_F32 || scale_dtype == GQ_BF16 ? GQ_OK : GQ_ERR_INVALID_ARG;
+}
+
+template <typename F> static gq_status with_scale_type(int t, F &&f) { return t == GQ_F32 ? f(float()) : f(bf16()); }
+
+}  // namespace gq
+
+using namespace gq;
+
+extern "C" {
+
+int64_t gq_w4_row_bytes(int64_t cols) { return cols < 0 || !matrix_fits(1, cols) ? 0 : (cols + 31) / 32 * 16; }
+
+gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype dtype, int group, void *codes_out, void *scales_out,
+                            gq_dtype scale_dtype, void *hip_stream)
+{
+    const gq_status st = check_weights(rows, cols, group, scale_dtype);
+    if (st != GQ_OK) return st;
+    if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return GQ_OK;
+    if (!aligned(w, 16) || !aligned(codes_out, 16) || !aligned(scales_out, 16)) return GQ_ERR_INVALID_ARG;
+    const int64_t groups = (cols + group - 1) / group, blocks = (rows * groups + kBlock - 1) / kBlock;
+    if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
+    return with_float_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        return with_scale_type(scale_dtype, [&](auto s) {
+            typedef decltype(s) S;
+            group_quantize_kernel<T, S><<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)w, rows, cols, group, (int)groups,
+                                                                                                 gq_w4_row_bytes(cols), (uint8_t *)codes_out, (S *)scales_out);
+            return launched();
+        });
+    });
+}
+
+gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, void *out,
+                              gq_dtype dtype, void *hip_stream)
+{
+    const gq_status st = check_weights(rows, cols, group, scale_dtype);
+    if (st != GQ_OK) return st;
+    if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return GQ_OK;
+    if (!aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, 16)) return GQ_ERR_INVALID_ARG;
+    const int64_t groups = (cols + group - 1) / group, blocks = (rows * ((cols + 7) / 8) + kBlock - 1) / kBlock;
+    if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
+    return with_float_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        return with_scale_type(scale_dtype, [&](auto s) {
+            typedef decltype(s) S;
+            group_dequantize_kernel<T, S><<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>(
+                (const uint32_t *)codes, (const S *)scales, rows, cols, group, (int)groups, gq_w4_row_bytes(cols) / 4, (T *)out);
+            return launched();
+        });
+    });
+}
+
+gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t m, gq_dtype x_dtype, const void *codes, const void *scales,
+                       gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, const void *bias, void *y, gq_dtype y_dtype,
+                       void *hip_stream)
+{
+    const gq_status st = check_weights(rows, cols, group, scale_dtype);
+    if (st != GQ_OK) return st;
+    if ((x_dtype != GQ_BF16 && x_dtype != GQ_F16 && x_dtype != GQ_I8) || !float_type(y_dtype) || (x_dtype == GQ_I8) != (x_scales != nullptr) ||
+        !matrix_fits(m, cols) || !matrix_fits(m, rows)) return GQ_ERR_INVALID_ARG;
+    if (m == 0 || rows == 0) return GQ_OK;
+    if (!aligned(y, 16) || !aligned_or_null(bias, 16) || (cols > 0 && (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16))) ||
+        !aligned_or_null(x_scales, 4)) return GQ_ERR_INVALID_ARG;
+    if (m > 65535 || !grid_fits(rows, 64)) return GQ_ERR_INVALID_ARG;
+    const int groups = (int)((cols + group - 1) / group);
+    return with_scale_type(scale_dtype, [&](auto s) {
+        typedef decltype(s) S;
+        auto go = [&](auto t) {
+            typedef decltype(t) X;
+            w4_matvec_kernel<X, S><<<dim3((unsigned)rows, (unsigned)m), 64, 0, (hipStream_t)hip_stream>>>(
+                (const X *)x, x_scales, (const uint32_t *)codes, (const S *)scales, rows, cols, group, groups, gq_w4_row_bytes(cols) / 4, bias, y, y_dtype);
+            return launched();
+        };
+        return x_dtype == GQ_BF16 ? go(bf16()) : x_dtype == GQ_F16 ? go(f16()) : go(int8_t());
+    });
+}
+
+}  // extern "C"
