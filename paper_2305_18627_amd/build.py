@@ -8,7 +8,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgqsgd.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("common.hip", "norm.hip", "quantize.hip", "aggregate.hip", "reduce.hip",
-                                           "sparse.hip", "pipeline.hip", "dropout.hip", "rms_norm.hip", "weights.hip")]
+                                           "sparse.hip", "pipeline.hip", "dropout.hip", "rms_norm.hip", "weights.hip", "matvec.hip")]
 MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 # for a test: gq_compact with a third of its spans mute (GQ_MUTE_SPANS in sparse.hip); nothing else loads it

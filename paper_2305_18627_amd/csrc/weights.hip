@@ -1,4 +1,4 @@
-// 4-bit weights under group scales: making them, unfolding them, and their product with rows of activations.
+// 4-bit weights under group scales: making them and unfolding them.
 // The contract of the entry points is stated in include/gqsgd.h.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -73,41 +73,6 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
     store8(out + row * cols + c, (int)(cols - c < 8 ? cols - c : 8), v);
 }
 
-// A wave per element of y.
-template <typename X, typename S>
-__global__ void __launch_bounds__(64)
-w4_matvec_kernel(const X *x, const float *x_scales, const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, int group, int groups,
-                 int64_t row_words, const void *bias, void *y, int y_dtype)
-{
-    const int64_t r = blockIdx.x, m = blockIdx.y;
-    double sum = 0.0;
-    for (int64_t c = threadIdx.x * 8; c < cols; c += 64 * 8) {
-        const uint32_t word = codes[r * row_words + c / 8];
-        float s = 0.0f, t = 0.0f;
-        for (int i = 0; i < 8 && c + i < cols; i++) {
-            const float xv = (float)x[m * cols + c + i];
-            s += xv * (float)(24 + ((int)(word << (28 - 4 * i)) >> 28));
-            t += xv;
-        }
-        sum += (double)(s - 24.0f * t) * (double)(float)scales[r * groups + c / group];
-    }
-    float v = (float)wave_sum(sum);
-    if (x_scales) v *= x_scales[m];
-    if (threadIdx.x != 0) return;
-    const int64_t at = m * rows + r;
-    if (y_dtype == GQ_F32) ((float *)y)[at] = v + (bias ? ((const float *)bias)[r] : 0.0f);
-    if (y_dtype == GQ_BF16) ((bf16 *)y)[at] = (bf16)(v + (bias ? (float)((const bf16 *)bias)[r] : 0.0f));
-    if (y_dtype == GQ_F16) ((f16 *)y)[at] = (f16)(v + (bias ? (float)((const f16 *)bias)[r] : 0.0f));
-}
-
-static gq_status check_weights(int64_t rows, int64_t cols, int group, int scale_dtype)
-{
-    if (!matrix_fits(rows, cols) || (group != 32 && group != 64 && group != 128)) return GQ_ERR_INVALID_ARG;
-    return scale_dtype == GQ_F32 || scale_dtype == GQ_BF16 ? GQ_OK : GQ_ERR_INVALID_ARG;
-}
-
-template <typename F> static gq_status with_scale_type(int t, F &&f) { return t == GQ_F32 ? f(float()) : f(bf16()); }
-
 }  // namespace gq
 
 using namespace gq;
@@ -155,31 +120,6 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
                 (const uint32_t *)codes, (const S *)scales, rows, cols, group, (int)groups, gq_w4_row_bytes(cols) / 4, (T *)out);
             return launched();
         });
-    });
-}
-
-gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t m, gq_dtype x_dtype, const void *codes, const void *scales,
-                       gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, const void *bias, void *y, gq_dtype y_dtype,
-                       void *hip_stream)
-{
-    const gq_status st = check_weights(rows, cols, group, scale_dtype);
-    if (st != GQ_OK) return st;
-    if ((x_dtype != GQ_BF16 && x_dtype != GQ_F16 && x_dtype != GQ_I8) || !float_type(y_dtype) || (x_dtype == GQ_I8) != (x_scales != nullptr) ||
-        !matrix_fits(m, cols) || !matrix_fits(m, rows)) return GQ_ERR_INVALID_ARG;
-    if (m == 0 || rows == 0) return GQ_OK;
-    if (!aligned(y, 16) || !aligned_or_null(bias, 16) || (cols > 0 && (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16))) ||
-        !aligned_or_null(x_scales, 4)) return GQ_ERR_INVALID_ARG;
-    if (m > 65535 || !grid_fits(rows, 64)) return GQ_ERR_INVALID_ARG;
-    const int groups = (int)((cols + group - 1) / group);
-    return with_scale_type(scale_dtype, [&](auto s) {
-        typedef decltype(s) S;
-        auto go = [&](auto t) {
-            typedef decltype(t) X;
-            w4_matvec_kernel<X, S><<<dim3((unsigned)rows, (unsigned)m), 64, 0, (hipStream_t)hip_stream>>>(
-                (const X *)x, x_scales, (const uint32_t *)codes, (const S *)scales, rows, cols, group, groups, gq_w4_row_bytes(cols) / 4, bias, y, y_dtype);
-            return launched();
-        };
-        return x_dtype == GQ_BF16 ? go(bf16()) : x_dtype == GQ_F16 ? go(f16()) : go(int8_t());
     });
 }
 
