@@ -33,7 +33,13 @@ template <typename V, uint32_t ONE, int TOP, uint32_t MINUS> struct Act16 {
         return __builtin_bit_cast(Operand, r);
     }
     static __device__ __forceinline__ Operand minus24() { return __builtin_bit_cast(Operand, u32x4{MINUS, MINUS, MINUS, MINUS}); }
-    static constexpr int kOrder[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+    // eight activations as they lie in memory, and in the order of unfold()
+    typedef u32x4 Raw;
+    typedef uint16_t Bits;
+    static __device__ __forceinline__ Raw ordered(Raw v)
+    {
+        return Raw{(v.x & 0xFFFFu) | (v.z << 16), (v.x >> 16) | (v.z & 0xFFFF0000u), (v.y & 0xFFFFu) | (v.w << 16), (v.y >> 16) | (v.w & 0xFFFF0000u)};
+    }
 };
 template <> struct Act<bf16> : Act16<bf16x8, 0x41804180u, 3, 0xC1C0C1C0u> {
     static __device__ __forceinline__ Sum product(Operand a, Operand b, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -52,7 +58,12 @@ template <> struct Act<int8_t> {
     }
     static __device__ __forceinline__ Sum product(Operand a, Operand b, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ Operand minus24() { return 0; }
-    static constexpr int kOrder[8] = {0, 2, 4, 6, 1, 3, 5, 7};
+    typedef u32x2 Raw;
+    typedef uint8_t Bits;
+    static __device__ __forceinline__ Raw ordered(Raw v)
+    {
+        return Raw{__builtin_amdgcn_perm(v.y, v.x, 0x06040200u), __builtin_amdgcn_perm(v.y, v.x, 0x07050301u)};
+    }
 };
 
 // d[j] of lane group q (lanes 16 q .. 16 q + 15) becomes d[q] of lane group j
@@ -72,105 +83,125 @@ struct MatvecArgs {
     const void *scales, *bias;
     void *y;
     int64_t row_bytes;
-    int m, rows, cols, groups, y_dtype, stage_shift;     // a stage of x in LDS: 2^stage_shift columns
+    int m, rows, cols, groups, y_dtype;
+    int row_shift;        // a row of staged x in LDS has 2^row_shift columns
 };
 
-// A workgroup of WN x WK waves owns WN * RT * 16 rows of the weights and up to MT * 16 rows of x; the WK waves share out the
-// columns, 128 U at a time, and their sums are joined in LDS at the end.  x is staged in LDS, a stage at a time.
-template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U>
+// A workgroup of WN x WK waves owns WN * RT * 16 rows of the weights at a time and up to MT * 16 rows of x; the WK waves share out
+// the columns, 128 U at a time (a step), and their sums are joined in LDS at a tile's end.  x is staged in LDS: RESIDENT, all of
+// it, once, for all tiles of rows that the workgroup takes in turn; otherwise a step's columns at a time into two buffers in
+// turn, the next step's loads in flight meanwhile, and the workgroup takes one tile.
+template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U, bool RESIDENT>
 __global__ void __launch_bounds__(64 * WN * WK)
 w4_matvec_kernel(MatvecArgs p)
 {
     typedef Act<X> A;
     typedef typename A::Operand Operand;
     typedef typename A::Sum Sum;
+    typedef typename A::Raw Raw;
+    typedef typename A::Bits Bits;
     constexpr int kThreads = 64 * WN * WK, kUnit = 8 * (int)sizeof(X), kSwizzle = 128 / kUnit - 1;
-    constexpr int kGroups = 128 / GROUP, kBlocks = GROUP / 32;
+    constexpr int kGroups = 128 / GROUP, kBlocks = GROUP / 32, kStep = 128 * U * WK;
+    constexpr int kPerWave = MT * RT * 256, kPart = WN * WK * kPerWave;            // floats of the waves' sums
+    constexpr int kBuffer = MT * 16 * kStep * (int)sizeof(X);
+    constexpr int kAhead = MT * 16 * (kStep / 8) / kThreads;                       // units of a step's x per lane
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wk = wave % WK, wn = wave / WK;
     const int i16 = lane & 15, q = lane >> 4;
-    const int first_row = (blockIdx.x * WN + wn) * RT * 16, first_m = blockIdx.y * MT * 16;
-    const int m_rows = min(p.m - first_m, MT * 16);
+    const int first_m = blockIdx.y * MT * 16, m_rows = min(p.m - first_m, MT * 16);
     const X *x = (const X *)p.x + (int64_t)first_m * p.cols;
+    const int tiles = (p.rows + WN * RT * 16 - 1) / (WN * RT * 16), steps = (p.cols + kStep - 1) / kStep;
 
-    const uint8_t *code_row[RT];
-    const S *scale_row[RT];
+    // ---- x: units of eight columns, in the order in which the codes unfold ----
+    auto load_unit = [&](int row, int c) {
+        Raw v;
+        const X *at = x + (int64_t)row * p.cols + c;
+        if (c + 8 <= p.cols) {
+            __builtin_memcpy(&v, at, sizeof(v));
+        } else {
+            constexpr int kBits = 8 * (int)sizeof(X), kWord = 32 / kBits;
+            v = Raw{};
 #pragma unroll
-    for (int t = 0; t < RT; t++) {
-        const int64_t r = min(first_row + 16 * t + i16, p.rows - 1);    // rows past the last one: its codes again, never stored
-        code_row[t] = p.codes + r * p.row_bytes;
-        scale_row[t] = (const S *)p.scales + r * p.groups;
+            for (int i = 0; i < 8; i++)
+                if (c + i < p.cols) v[i / kWord] |= (uint32_t) reinterpret_cast<const Bits *>(at)[i] << (kBits * (i % kWord));
+        }
+        return v;
+    };
+    auto store_unit = [&](uint8_t *to, int row, int unit, int shift, Raw v) {
+        *reinterpret_cast<Raw *>(to + ((row << shift) + (unit ^ (row & kSwizzle))) * kUnit) = A::ordered(v);
+    };
+    const int shift = RESIDENT ? p.row_shift - 3 : __builtin_ctz(kStep / 8);       // of units a row
+    // where a lane finds operand A: unit 16 chunk + (4 j + q), or (4 q + j) for groups of 128, of its row; a chunk is 128 columns
+    int from[MT][4];
+#pragma unroll
+    for (int i = 0; i < MT; i++) {
+        const int r = min(16 * i + i16, m_rows - 1);
+#pragma unroll
+        for (int j = 0; j < 4; j++) from[i][j] = ((r << shift) + ((GROUP < 128 ? 4 * j + q : 4 * q + j) ^ (r & kSwizzle))) * kUnit;
     }
+
+    // ---- codes and scales of a step: 16 bytes a lane and chunk ----
     struct Fetched { u32x4 w[U][RT]; float s[U][RT][kGroups]; };
-    const int last_block = (p.cols + 31) / 32 - 1, steps = (p.cols + 128 * U * WK - 1) / (128 * U * WK);
-    auto fetch = [&](int step, Fetched &f) {
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int c = ((step * WK + wk) * U + u) * 128;
-            // 16 bytes of codes a lane; past the row's end the last ones again, where x is zero
-            const int b = min(c / 32 + q, last_block);
+    const uint32_t scale_bytes = (uint32_t)(p.groups * (int)sizeof(S));
+    auto fetch = [&](int tile, int step, Fetched &f) {
+        // a wave whose rows all lie past the last one reads that one
+        const int first = min((tile * WN + wn) * RT * 16, p.rows - 1), c = (step * WK + wk) * U * 128;
+        // the wave's first row and column are the same for all lanes; what differs is a lane's row within the tile.  Rows past
+        // the last one: its codes again, never stored
+        const uint8_t *codes = p.codes + (int64_t)first * p.row_bytes + c / 2;
+        const uint8_t *scales = (const uint8_t *)p.scales + ((int64_t)first * p.groups + c / GROUP) * (int)sizeof(S);
+        const int last = p.rows - 1 - first;
+        if (c + U * 128 <= p.cols) {
 #pragma unroll
             for (int t = 0; t < RT; t++) {
-                f.w[u][t] = *reinterpret_cast<const u32x4 *>(code_row[t] + 16 * (int64_t)b);
+                const uint32_t r = (uint32_t)min(16 * t + i16, last);
+                const uint32_t at = r * (uint32_t)p.row_bytes + 16u * (uint32_t)q;
 #pragma unroll
-                for (int g = 0; g < kGroups; g++) {
-                    const int at = c / GROUP + g;
-                    const float s = (float)scale_row[t][min(at, p.groups - 1)];
-                    f.s[u][t][g] = at < p.groups ? s : 0.0f;
+                for (int u = 0; u < U; u++) f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + at + 64 * u);
+                struct { S e[U * kGroups]; } s;
+                __builtin_memcpy(&s, scales + r * scale_bytes, sizeof(s));
+#pragma unroll
+                for (int u = 0; u < U; u++)
+#pragma unroll
+                    for (int g = 0; g < kGroups; g++) f.s[u][t][g] = (float)s.e[u * kGroups + g];
+            }
+        } else {
+            // the row's end: past it the last codes again, where x is zero, and scales of zero
+#pragma unroll
+            for (int t = 0; t < RT; t++) {
+                const uint32_t r = (uint32_t)min(16 * t + i16, last);
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int b = min(c / 32 + 4 * u + q, (p.cols - 1) / 32) - c / 32;
+                    f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (int64_t)r * p.row_bytes + 16 * b);
+#pragma unroll
+                    for (int g = 0; g < kGroups; g++) {
+                        const int at = min(c / GROUP + u * kGroups + g, p.groups - 1) - c / GROUP;
+                        const float s = (float)reinterpret_cast<const S *>(scales + (int64_t)r * scale_bytes)[at];
+                        f.s[u][t][g] = c / GROUP + u * kGroups + g < p.groups ? s : 0.0f;
+                    }
                 }
             }
         }
     };
 
-    const int stage_cols = 1 << p.stage_shift, units_shift = p.stage_shift - 3;
-    auto stage = [&](int first_col) {
-        for (int u = threadIdx.x; u < (m_rows << units_shift); u += kThreads) {
-            const int row = u >> units_shift, unit = u & ((1 << units_shift) - 1), c = first_col + 8 * unit;
-            Eight<X> v, o;
-            const X *at = x + (int64_t)row * p.cols + c;
-            if (c + 8 <= p.cols) {
-                __builtin_memcpy(&v, at, sizeof(v));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) v.e[i] = c + i < p.cols ? at[i] : (X)0;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; i++) o.e[i] = v.e[A::kOrder[i]];
-            *reinterpret_cast<Operand *>(lds + ((row << units_shift) + (unit ^ (row & kSwizzle))) * kUnit) = __builtin_bit_cast(Operand, o);
-        }
-    };
-    int lds_row[MT], lds_mask[MT];
-#pragma unroll
-    for (int t = 0; t < MT; t++) {
-        const int r = min(16 * t + i16, m_rows - 1);
-        lds_row[t] = r << units_shift;
-        lds_mask[t] = r & kSwizzle;
-    }
-
     f32x4 acc[MT][RT];
+    auto clear = [&] {
 #pragma unroll
-    for (int i = 0; i < MT; i++)
+        for (int i = 0; i < MT; i++)
 #pragma unroll
-        for (int t = 0; t < RT; t++) acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    Fetched now, next;
-    if (steps > 0) fetch(0, now);
-    const int steps_per_stage = stage_cols / (128 * U * WK);
-    for (int step = 0; step < steps; step++) {
-        if (step % steps_per_stage == 0) {
-            if (step) __syncthreads();
-            stage(step * 128 * U * WK);
-            __syncthreads();
-        }
-        if (step + 1 < steps) fetch(step + 1, next);
+            for (int t = 0; t < RT; t++) acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    // a step's products; `staged`: where its first column is
+    auto multiply = [&](const Fetched &f, const uint8_t *staged) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int in_stage = (((step % steps_per_stage) * WK + wk) * U + u) * 128;
+            const uint8_t *chunk = staged + (wk * U + u) * 16 * kUnit;
             uint32_t d[RT][4];
 #pragma unroll
             for (int t = 0; t < RT; t++) {
 #pragma unroll
-                for (int j = 0; j < 4; j++) d[t][j] = now.w[u][t][j];
+                for (int j = 0; j < 4; j++) d[t][j] = f.w[u][t][j];
                 // operand j of the whole wave has to lie within a group: a group of 128 takes word j of each lane as it comes
                 if (GROUP < 128) transpose4(d[t]);
             }
@@ -183,8 +214,7 @@ w4_matvec_kernel(MatvecArgs p)
                     start[i] = Sum{};
 #pragma unroll
                     for (int j = 0; j < kBlocks; j++) {
-                        const int unit = in_stage / 8 + (GROUP < 128 ? 4 * (g * kBlocks + j) + q : 4 * q + j);
-                        a[i][j] = *reinterpret_cast<const Operand *>(lds + (lds_row[i] + (unit ^ lds_mask[i])) * kUnit);
+                        a[i][j] = *reinterpret_cast<const Operand *>(chunk + from[i][g * kBlocks + j]);
                         if (A::kMoved) start[i] = A::product(a[i][j], A::minus24(), start[i]);
                     }
                 }
@@ -199,60 +229,156 @@ w4_matvec_kernel(MatvecArgs p)
 #pragma unroll
                         for (int j = 0; j < kBlocks; j++) s = A::product(a[i][j], b[j], s);
 #pragma unroll
-                        for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], now.s[u][t][g], acc[i][t][r]);
+                        for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], f.s[u][t][g], acc[i][t][r]);
                     }
                 }
+                // the groups one after another: all at once they hold more than the registers that there are
+                if (MT * RT > 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        now = next;
-    }
+    };
+    // the waves that shared out the columns leave their sums in `part`; element (m 4 q + r, row i16) of a tile is lane 16 q + i16's r-th
+    auto leave = [&](float *part) {
+#pragma unroll
+        for (int i = 0; i < MT; i++)
+#pragma unroll
+            for (int t = 0; t < RT; t++)
+                *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + ((i * RT + t) * 64 + lane) * 4) = acc[i][t];
+    };
+    auto join = [&](const float *part, int tile_of_rows) {
+        for (int e = threadIdx.x; e < WN * kPerWave; e += kThreads) {
+            // e: (wave of rows, tile, m within it, row within it), the row fastest
+            const int w = e / kPerWave, tile = e % kPerWave / 256, mi = e % 256 / 16, ri = e % 16;
+            const int mm = first_m + tile / RT * 16 + mi, row = (tile_of_rows * WN + w) * RT * 16 + tile % RT * 16 + ri;
+            if (mm >= p.m || row >= p.rows) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
+            if (p.x_scales) v *= A::kUnit * p.x_scales[mm];
+            const int64_t at = (int64_t)mm * p.rows + row;
+            if (p.y_dtype == GQ_F32) ((float *)p.y)[at] = p.bias ? v + ((const float *)p.bias)[row] : v;
+            else if (p.y_dtype == GQ_BF16) ((bf16 *)p.y)[at] = (bf16)(p.bias ? v + (float)((const bf16 *)p.bias)[row] : v);
+            else ((f16 *)p.y)[at] = (f16)(p.bias ? v + (float)((const f16 *)p.bias)[row] : v);
+        }
+    };
 
-    // join the waves that shared out the columns; element (m 4 q + r, row i16) of a tile is lane 16 q + i16's r-th
-    __syncthreads();
-    float *part = reinterpret_cast<float *>(lds);
-    constexpr int kPerWave = MT * RT * 256;
+    Fetched now, next;
+    if constexpr (RESIDENT) {
+        // the first units of x are asked for before the codes: loads come back in order, and x is wanted first
+        const int units = m_rows << shift;
+        constexpr int kFirst = 2;
+        Raw v[kFirst];
 #pragma unroll
-    for (int i = 0; i < MT; i++)
+        for (int i = 0; i < kFirst; i++) {
+            const int u = min((int)threadIdx.x + i * kThreads, units - 1);
+            v[i] = load_unit(u >> shift, (u & ((1 << shift) - 1)) * 8);
+        }
+        if (steps > 0) fetch(blockIdx.x, 0, now);
 #pragma unroll
-        for (int t = 0; t < RT; t++)
-            *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + ((i * RT + t) * 64 + lane) * 4) = acc[i][t];
-    __syncthreads();
-    for (int e = threadIdx.x; e < WN * kPerWave; e += kThreads) {
-        // e: (wave of rows, tile, m within it, row within it), the row fastest
-        const int w = e / kPerWave, tile = e % kPerWave / 256, mi = e % 256 / 16, ri = e % 16;
-        const int mm = first_m + tile / RT * 16 + mi, row = (blockIdx.x * WN + w) * RT * 16 + tile % RT * 16 + ri;
-        if (mm >= p.m || row >= p.rows) continue;
-        float v = 0.0f;
+        for (int i = 0; i < kFirst; i++) {
+            const int u = (int)threadIdx.x + i * kThreads;
+            if (u < units) store_unit(lds, u >> shift, u & ((1 << shift) - 1), shift, v[i]);
+        }
+        for (int u = threadIdx.x + kFirst * kThreads; u < units; u += kThreads)
+            store_unit(lds, u >> shift, u & ((1 << shift) - 1), shift, load_unit(u >> shift, (u & ((1 << shift) - 1)) * 8));
+        __syncthreads();
+        float *parts = reinterpret_cast<float *>(lds + units * kUnit);             // two, in turn
+        int turn = 0;
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+            clear();
+            for (int step = 0; step < steps; step++) {
+                const bool more = step + 1 < steps;
+                if (more || tile + (int)gridDim.x < tiles) fetch(more ? tile : tile + gridDim.x, more ? step + 1 : 0, next);
+                multiply(now, lds + step * (kStep / 8) * kUnit);
+                now = next;
+            }
+            // one barrier a tile: who writes a part again has passed the next tile's, and so have all who read it
+            leave(parts + turn * kPart);
+            __syncthreads();
+            join(parts + turn * kPart, tile);
+        }
+    } else {
+        // a lane's units are in one column of units, kRowsApart rows apart
+        constexpr int kRowUnits = kStep / 8, kRowsApart = kThreads / kRowUnits;
+        static_assert(kThreads % kRowUnits == 0 && kAhead * kRowsApart == MT * 16, "units of a step");
+        const int unit = threadIdx.x % kRowUnits, row0 = threadIdx.x / kRowUnits;
+        const uint32_t x_at = (uint32_t)(row0 * p.cols + 8 * unit);
+        Raw ahead[kAhead];
+        auto ask = [&](int step) {
+            const X *first = x + step * kStep;
+            if ((step + 1) * kStep <= p.cols) {
 #pragma unroll
-        for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
-        if (p.x_scales) v *= A::kUnit * p.x_scales[mm];
-        const int64_t at = (int64_t)mm * p.rows + row;
-        if (p.y_dtype == GQ_F32) ((float *)p.y)[at] = p.bias ? v + ((const float *)p.bias)[row] : v;
-        else if (p.y_dtype == GQ_BF16) ((bf16 *)p.y)[at] = (bf16)(p.bias ? v + (float)((const bf16 *)p.bias)[row] : v);
-        else ((f16 *)p.y)[at] = (f16)(p.bias ? v + (float)((const f16 *)p.bias)[row] : v);
+                for (int i = 0; i < kAhead; i++)
+                    if (row0 + i * kRowsApart < m_rows) __builtin_memcpy(&ahead[i], first + i * kRowsApart * p.cols + x_at, sizeof(Raw));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kAhead; i++)
+                    if (row0 + i * kRowsApart < m_rows) ahead[i] = load_unit(row0 + i * kRowsApart, step * kStep + 8 * unit);
+            }
+        };
+        auto put = [&](int step) {
+            uint8_t *to = lds + (step & 1) * kBuffer;
+#pragma unroll
+            for (int i = 0; i < kAhead; i++)
+                if (row0 + i * kRowsApart < m_rows) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
+        };
+        clear();
+        if (steps > 0) {
+            ask(0);
+            fetch(blockIdx.x, 0, now);
+            put(0);
+        }
+        __syncthreads();
+        for (int step = 0; step < steps; step++) {
+            const bool more = step + 1 < steps;
+            if (more) {
+                ask(step + 1);
+                fetch(blockIdx.x, step + 1, next);
+            }
+            multiply(now, lds + (step & 1) * kBuffer);
+            if (more) put(step + 1);                     // last read two steps ago, before the barrier that ended that step
+            now = next;
+            __syncthreads();
+        }
+        float *part = reinterpret_cast<float *>(lds);
+        leave(part);
+        __syncthreads();
+        join(part, blockIdx.x);
     }
 }
 
-template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U>
+constexpr int kLds = 64 * 1024;
+constexpr int kResidentGrid = 768;
+
+template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U, bool RESIDENT>
 static gq_status launch_matvec(MatvecArgs p, hipStream_t stream)
 {
-    constexpr int kStep = 128 * U * WK, kLimit = 64 * 1024;
-    const int m_rows = p.m < MT * 16 ? p.m : MT * 16;
-    static_assert(MT * 16 * kStep * (int)sizeof(X) <= kLimit && WN * WK * MT * RT * 1024 <= kLimit, "LDS");
-    p.stage_shift = __builtin_ctz(kStep);
-    while ((1 << p.stage_shift) < p.cols && (m_rows << (p.stage_shift + 1)) * (int)sizeof(X) <= kLimit) p.stage_shift++;
-    const unsigned staged = (unsigned)(m_rows << p.stage_shift) * (unsigned)sizeof(X), joined = WN * WK * MT * RT * 1024;
-    const int64_t bx = ((int64_t)p.rows + WN * RT * 16 - 1) / (WN * RT * 16), by = ((int64_t)p.m + MT * 16 - 1) / (MT * 16);
+    constexpr int kStep = 128 * U * WK, kParts = WN * WK * MT * RT * 1024, kRows = WN * RT * 16;
+    int64_t bx = ((int64_t)p.rows + kRows - 1) / kRows;
+    const int64_t by = ((int64_t)p.m + MT * 16 - 1) / (MT * 16);
+    unsigned lds;
+    if (RESIDENT) {
+        lds = (unsigned)((p.m << p.row_shift) * (int)sizeof(X) + 2 * kParts);
+        if (bx > kResidentGrid) bx = kResidentGrid;
+    } else {
+        lds = 2 * MT * 16 * kStep * (int)sizeof(X);
+        if (lds < kParts) lds = kParts;
+    }
     if (!grid_fits(bx, 64 * WN * WK) || by > 65535) return GQ_ERR_INVALID_ARG;
-    w4_matvec_kernel<X, S, GROUP, MT, RT, WN, WK, U><<<dim3((unsigned)bx, (unsigned)by), 64 * WN * WK, staged > joined ? staged : joined, stream>>>(p);
+    w4_matvec_kernel<X, S, GROUP, MT, RT, WN, WK, U, RESIDENT><<<dim3((unsigned)bx, (unsigned)by), 64 * WN * WK, lds, stream>>>(p);
     return launched();
 }
 
-template <typename X, typename S, int GROUP> static gq_status matvec_by_rows(const MatvecArgs &p, hipStream_t stream)
+template <typename X, typename S, int GROUP> static gq_status matvec_by_rows(MatvecArgs p, hipStream_t stream)
 {
-    if (p.m <= 16) return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2>(p, stream);
-    if (p.m <= 32) return launch_matvec<X, S, GROUP, 2, 2, 2, 4, 2>(p, stream);
-    return launch_matvec<X, S, GROUP, 4, 2, 2, 4, 1>(p, stream);
+    if (p.m <= 16) {
+        p.row_shift = 11;                                                          // whole steps of 2048 columns
+        while ((1 << p.row_shift) < p.cols) p.row_shift++;
+        if (((int64_t)p.m << p.row_shift) * (int)sizeof(X) <= kLds - 16 * 1024) return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2, true>(p, stream);
+        return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2, false>(p, stream);
+    }
+    if (p.m <= 32) return launch_matvec<X, S, GROUP, 2, 2, 2, 4, 2, false>(p, stream);
+    return launch_matvec<X, S, GROUP, 4, 2, 2, 4, 1, false>(p, stream);
 }
 
 }  // namespace gq
