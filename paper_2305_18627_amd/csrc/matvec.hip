@@ -127,18 +127,40 @@ w4_matvec_kernel(MatvecArgs p)
         }
         return v;
     };
+    // v without its first `over` elements, zeros behind; v itself for over <= 0
+    auto drop_low = [&](Raw v, int over) {
+        if (over <= 0) return v;
+        constexpr int kWords = sizeof(Raw) / 4, kBits = 8 * (int)sizeof(X);
+        const int bits = min(over, 8) * kBits, words = bits / 32, rest = bits % 32;
+        uint32_t w[2 * kWords + 1];
+#pragma unroll
+        for (int i = 0; i <= 2 * kWords; i++) w[i] = i < kWords ? v[i] : 0u;
+        Raw o;
+#pragma unroll
+        for (int i = 0; i < kWords; i++) {
+            uint32_t lo = 0, hi = 0;
+#pragma unroll
+            for (int k = 0; k <= kWords; k++) {
+                lo = words == k ? w[i + k] : lo;
+                hi = words == k ? w[i + k + 1] : hi;
+            }
+            o[i] = (uint32_t)((((uint64_t)hi << 32) | lo) >> rest);
+        }
+        return o;
+    };
     auto store_unit = [&](uint8_t *to, int row, int unit, int shift, Raw v) {
         *reinterpret_cast<Raw *>(to + ((row << shift) + (unit ^ (row & kSwizzle))) * kUnit) = A::ordered(v);
     };
     const int shift = RESIDENT ? p.row_shift - 3 : __builtin_ctz(kStep / 8);       // of units a row
-    // where a lane finds operand A: unit 16 chunk + (4 j + q), or (4 q + j) for groups of 128, of its row; a chunk is 128 columns
-    int from[MT][4];
+    // where a lane finds operand A: unit 16 chunk + (4 j + q), or (4 q + j) for groups of 128, of its row; a chunk is 128 columns.
+    // Rows of x that are not there are the last one again and end in rows of y that are not there.
+    int from[4];
 #pragma unroll
-    for (int i = 0; i < MT; i++) {
-        const int r = min(16 * i + i16, m_rows - 1);
-#pragma unroll
-        for (int j = 0; j < 4; j++) from[i][j] = ((r << shift) + ((GROUP < 128 ? 4 * j + q : 4 * q + j) ^ (r & kSwizzle))) * kUnit;
+    for (int j = 0; j < 4; j++) {
+        const int r = RESIDENT ? min(i16, m_rows - 1) : i16;
+        from[j] = ((r << shift) + ((GROUP < 128 ? 4 * j + q : 4 * q + j) ^ (r & kSwizzle))) * kUnit;
     }
+    constexpr int kTileBytes = 16 * kStep * (int)sizeof(X);                        // of 16 rows of x, streamed
 
     // ---- codes and scales of a step: 16 bytes a lane and chunk ----
     struct Fetched { u32x4 w[U][RT]; float s[U][RT][kGroups]; };
@@ -151,7 +173,7 @@ w4_matvec_kernel(MatvecArgs p)
         const uint8_t *codes = p.codes + (int64_t)first * p.row_bytes + c / 2;
         const uint8_t *scales = (const uint8_t *)p.scales + ((int64_t)first * p.groups + c / GROUP) * (int)sizeof(S);
         const int last = p.rows - 1 - first;
-        if (c + U * 128 <= p.cols) {
+        if (RESIDENT && c + U * 128 <= p.cols) {
 #pragma unroll
             for (int t = 0; t < RT; t++) {
                 const uint32_t r = (uint32_t)min(16 * t + i16, last);
@@ -166,18 +188,19 @@ w4_matvec_kernel(MatvecArgs p)
                     for (int g = 0; g < kGroups; g++) f.s[u][t][g] = (float)s.e[u * kGroups + g];
             }
         } else {
-            // the row's end: past it the last codes again, where x is zero, and scales of zero
+            // past the row's end the last codes again, where x is zero, and scales of zero.  Streamed, all steps come here: a second
+            // way through costs more registers than this
 #pragma unroll
             for (int t = 0; t < RT; t++) {
                 const uint32_t r = (uint32_t)min(16 * t + i16, last);
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     const int b = min(c / 32 + 4 * u + q, (p.cols - 1) / 32) - c / 32;
-                    f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (int64_t)r * p.row_bytes + 16 * b);
+                    f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (int)(r * (uint32_t)p.row_bytes) + 16 * b);
 #pragma unroll
                     for (int g = 0; g < kGroups; g++) {
                         const int at = min(c / GROUP + u * kGroups + g, p.groups - 1) - c / GROUP;
-                        const float s = (float)reinterpret_cast<const S *>(scales + (int64_t)r * scale_bytes)[at];
+                        const float s = (float)*reinterpret_cast<const S *>(scales + at * (int)sizeof(S) + r * scale_bytes);
                         f.s[u][t][g] = c / GROUP + u * kGroups + g < p.groups ? s : 0.0f;
                     }
                 }
@@ -214,7 +237,7 @@ w4_matvec_kernel(MatvecArgs p)
                     start[i] = Sum{};
 #pragma unroll
                     for (int j = 0; j < kBlocks; j++) {
-                        a[i][j] = *reinterpret_cast<const Operand *>(chunk + from[i][g * kBlocks + j]);
+                        a[i][j] = *reinterpret_cast<const Operand *>(chunk + from[g * kBlocks + j] + i * kTileBytes);
                         if (A::kMoved) start[i] = A::product(a[i][j], A::minus24(), start[i]);
                     }
                 }
@@ -232,8 +255,15 @@ w4_matvec_kernel(MatvecArgs p)
                         for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], f.s[u][t][g], acc[i][t][r]);
                     }
                 }
-                // the groups one after another: all at once they hold more than the registers that there are
-                if (MT * RT > 1) __builtin_amdgcn_sched_barrier(0);
+                // the groups one after another, sums and all: left to itself the compiler moves all sums behind all products, and
+                // the products of all groups at once are more than the registers that there are
+                if (MT * RT > 1) {
+#pragma unroll
+                    for (int i = 0; i < MT; i++)
+#pragma unroll
+                        for (int t = 0; t < RT; t++) asm volatile("" : "+v"(acc[i][t]));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
     };
@@ -298,29 +328,34 @@ w4_matvec_kernel(MatvecArgs p)
             join(parts + turn * kPart, tile);
         }
     } else {
-        // a lane's units are in one column of units, kRowsApart rows apart
+        // a lane's units are in one column of units, kRowsApart rows apart; rows that are not there hold the last one again
         constexpr int kRowUnits = kStep / 8, kRowsApart = kThreads / kRowUnits;
         static_assert(kThreads % kRowUnits == 0 && kAhead * kRowsApart == MT * 16, "units of a step");
         const int unit = threadIdx.x % kRowUnits, row0 = threadIdx.x / kRowUnits;
-        const uint32_t x_at = (uint32_t)(row0 * p.cols + 8 * unit);
         Raw ahead[kAhead];
+        // a unit that runs over the row's end (or lies past it) is read so that it ends there, and moved into place in put()
         auto ask = [&](int step) {
-            const X *first = x + step * kStep;
-            if ((step + 1) * kStep <= p.cols) {
+            const int c = min(step * kStep + 8 * unit, p.cols - 8);
+            if (p.cols >= 8) {
 #pragma unroll
                 for (int i = 0; i < kAhead; i++)
-                    if (row0 + i * kRowsApart < m_rows) __builtin_memcpy(&ahead[i], first + i * kRowsApart * p.cols + x_at, sizeof(Raw));
-            } else {
-#pragma unroll
-                for (int i = 0; i < kAhead; i++)
-                    if (row0 + i * kRowsApart < m_rows) ahead[i] = load_unit(row0 + i * kRowsApart, step * kStep + 8 * unit);
+                    __builtin_memcpy(&ahead[i], x + (uint32_t)(min(row0 + i * kRowsApart, m_rows - 1) * p.cols + c), sizeof(Raw));
             }
         };
         auto put = [&](int step) {
             uint8_t *to = lds + (step & 1) * kBuffer;
+            if (p.cols < 8) {
+                for (int i = 0; i < kAhead; i++)
+                    store_unit(to, row0 + i * kRowsApart, unit, shift, load_unit(min(row0 + i * kRowsApart, m_rows - 1), 8 * unit));
+                return;
+            }
+            if ((step + 1) * kStep > p.cols) {
+                const int over = step * kStep + 8 * unit - (p.cols - 8);           // elements to drop from the low end
 #pragma unroll
-            for (int i = 0; i < kAhead; i++)
-                if (row0 + i * kRowsApart < m_rows) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
+                for (int i = 0; i < kAhead; i++) ahead[i] = drop_low(ahead[i], over);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
         };
         clear();
         if (steps > 0) {
@@ -375,9 +410,9 @@ template <typename X, typename S, int GROUP> static gq_status matvec_by_rows(Mat
         p.row_shift = 11;                                                          // whole steps of 2048 columns
         while ((1 << p.row_shift) < p.cols) p.row_shift++;
         if (((int64_t)p.m << p.row_shift) * (int)sizeof(X) <= kLds - 16 * 1024) return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2, true>(p, stream);
-        return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2, false>(p, stream);
     }
-    if (p.m <= 32) return launch_matvec<X, S, GROUP, 2, 2, 2, 4, 2, false>(p, stream);
+    if (p.m <= 16 || p.rows <= 2048) return launch_matvec<X, S, GROUP, 1, 1, 4, 2, 4, false>(p, stream);
+    if (p.m <= 32) return launch_matvec<X, S, GROUP, 2, 2, 2, 4, 1, false>(p, stream);
     return launch_matvec<X, S, GROUP, 4, 2, 2, 4, 1, false>(p, stream);
 }
 
