@@ -16,9 +16,9 @@ dropout_kernel(const T *x, const T *residual, T *out, int64_t units, uint32_t pe
 {
     const int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (u >= units) return;
-    const int64_t row = u / per_row, unit = u - row * per_row;
-    const int64_t at = row * n + unit * 8;
-    const int64_t left = n - unit * 8;
+    const RowUnit ru = row_unit(blockIdx.x, per_row);
+    const int64_t at = ru.row * n + (int64_t)ru.unit * 8;
+    const int64_t left = n - (int64_t)ru.unit * 8;
     const int valid = left < 8 ? (int)left : 8;
     float v[8];
     load8(x + at, valid, v);

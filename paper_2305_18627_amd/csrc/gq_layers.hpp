@@ -45,6 +45,17 @@ template <typename T> __device__ __forceinline__ void store8(T *p, int valid, co
     }
 }
 
+// Row and unit within it of a workgroup's lane, where rows have `per_row` units: one 64-bit division a workgroup, on the scalar
+// unit, and a 32-bit one a lane.
+struct RowUnit { int64_t row; uint32_t unit; };
+__device__ __forceinline__ RowUnit row_unit(uint32_t block, uint32_t per_row)
+{
+    const uint64_t first = (uint64_t)block * kBlock, row = first / per_row;
+    const uint32_t at = (uint32_t)(first - row * per_row) + threadIdx.x;           // below 2^28 + 256 for every matrix that fits
+    const uint32_t more = at / per_row;
+    return {(int64_t)row + more, at - more * per_row};
+}
+
 // The dropout decision of gq_dropout_params, as the kernels take it.
 struct Drop {
     uint32_t k0, k1, worker;

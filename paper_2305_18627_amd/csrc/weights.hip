@@ -31,46 +31,59 @@ template <typename S> __device__ __forceinline__ GroupScale<S> group_scale(uint3
     return {stored, scale, inv};
 }
 
-// A lane per group.
-template <typename T, typename S>
+// A lane owns a unit of eight consecutive columns (16 or 32 bytes of weights, one word of codes), a group is 4, 8 or 16
+// neighbouring lanes: the maximum goes round them by DPP within a row of 16 lanes.  Units past the row's last column (a row
+// is padded to whole groups of units) hold zeros; those within the padding of the row's codes write them.  Bound by memory: read
+// once, written once.
+template <typename T, typename S, int GROUP>
 __global__ void __launch_bounds__(kBlock)
-group_quantize_kernel(const T *w, int64_t rows, int64_t cols, int group, int groups, int64_t row_bytes, uint8_t *codes, S *scales)
+group_quantize_kernel(const T *w, int64_t units, int64_t cols, uint32_t units_per_row, int groups, uint32_t row_words, uint32_t *codes, S *scales)
 {
     const int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (u >= rows * groups) return;
-    const int64_t row = u / groups, first = (u - row * groups) * group;
-    const T *p = w + row * cols + first;
-    const int valid = (int)(cols - first < group ? cols - first : group);
-    uint32_t m = 0;
-    for (int i = 0; i < valid; i++) m = max(m, __float_as_uint((float)p[i]) & 0x7FFFFFFFu);
-    const GroupScale<S> gs = group_scale<S>(m);
-    scales[u] = gs.stored;
-    uint8_t *out = codes + row * row_bytes + first / 2;
-    const int padded = (valid + 31) / 32 * 32;
-    for (int i = 0; i < padded; i += 2) {
-        uint32_t b = 0;
-        for (int k = 0; k < 2; k++) {
-            if (i + k >= valid || gs.inv == 0.0f) continue;
-            b |= ((uint32_t)(int)code_of_quotient((float)p[i + k], gs.scale, gs.inv) & 15u) << (4 * k);
-        }
-        out[i / 2] = (uint8_t)b;
+    const RowUnit at = row_unit(blockIdx.x, units_per_row);
+    const int64_t left = cols - (int64_t)at.unit * 8;
+    const int valid = u >= units || left <= 0 ? 0 : left < 8 ? (int)left : 8;
+    float v[8];
+    if (valid > 0) {
+        load8(w + at.row * cols + (int64_t)at.unit * 8, valid, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = 0.0f;
     }
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    m = max(m, dpp32<kDppQuadXor1>(m));
+    m = max(m, dpp32<kDppQuadXor2>(m));
+    if (GROUP >= 64) m = max(m, dpp32<kDppHalfMirror>(m));
+    if (GROUP >= 128) m = max(m, dpp32<kDppMirror>(m));
+    const GroupScale<S> gs = group_scale<S>(m);
+    if (u >= units) return;
+    uint32_t word = 0;
+    if (gs.inv != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) word |= ((uint32_t)(int)code_of_quotient(v[i], gs.scale, gs.inv) & 15u) << (4 * i);
+    }
+    if (at.unit < row_words) codes[at.row * row_words + at.unit] = word;
+    if (at.unit % (GROUP / 8) == 0) scales[at.row * groups + at.unit / (GROUP / 8)] = gs.stored;
 }
 
 // A lane per eight columns.
 template <typename T, typename S>
 __global__ void __launch_bounds__(kBlock)
-group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, int group, int groups, int64_t row_words, T *out)
+group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t units, int64_t cols, uint32_t units_per_row, int group_shift, int groups,
+                        uint32_t row_words, T *out)
 {
     const int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    const int64_t per_row = (cols + 7) / 8;
-    if (u >= rows * per_row) return;
-    const int64_t row = u / per_row, c = (u - row * per_row) * 8;
-    const uint32_t word = codes[row * row_words + c / 8];
-    const float scale = (float)scales[row * groups + c / group];
+    if (u >= units) return;
+    const RowUnit at = row_unit(blockIdx.x, units_per_row);
+    const int64_t c = (int64_t)at.unit * 8;
+    const uint32_t word = codes[at.row * row_words + at.unit];
+    const float scale = (float)scales[at.row * groups + (c >> group_shift)];
     float v[8];
+#pragma unroll
     for (int i = 0; i < 8; i++) v[i] = (float)((int)(word << (28 - 4 * i)) >> 28) * scale;
-    store8(out + row * cols + c, (int)(cols - c < 8 ? cols - c : 8), v);
+    store8(out + at.row * cols + c, (int)(cols - c < 8 ? cols - c : 8), v);
 }
 
 }  // namespace gq
@@ -89,14 +102,16 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
     if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return GQ_OK;
     if (!aligned(w, 16) || !aligned(codes_out, 16) || !aligned(scales_out, 16)) return GQ_ERR_INVALID_ARG;
-    const int64_t groups = (cols + group - 1) / group, blocks = (rows * groups + kBlock - 1) / kBlock;
+    // whole groups of units, whole words of codes
+    const int64_t per_row = ((cols + group - 1) / group * group) / 8, units = rows * per_row, blocks = (units + kBlock - 1) / kBlock;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         return with_scale_type(scale_dtype, [&](auto s) {
             typedef decltype(s) S;
-            group_quantize_kernel<T, S><<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)w, rows, cols, group, (int)groups,
-                                                                                                 gq_w4_row_bytes(cols), (uint8_t *)codes_out, (S *)scales_out);
+            auto kernel = group == 32 ? group_quantize_kernel<T, S, 32> : group == 64 ? group_quantize_kernel<T, S, 64> : group_quantize_kernel<T, S, 128>;
+            kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)w, units, cols, (uint32_t)per_row, (int)((cols + group - 1) / group),
+                                                                           (uint32_t)(gq_w4_row_bytes(cols) / 4), (uint32_t *)codes_out, (S *)scales_out);
             return launched();
         });
     });
@@ -110,14 +125,15 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
     if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return GQ_OK;
     if (!aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, 16)) return GQ_ERR_INVALID_ARG;
-    const int64_t groups = (cols + group - 1) / group, blocks = (rows * ((cols + 7) / 8) + kBlock - 1) / kBlock;
+    const int64_t per_row = (cols + 7) / 8, units = rows * per_row, blocks = (units + kBlock - 1) / kBlock;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         return with_scale_type(scale_dtype, [&](auto s) {
             typedef decltype(s) S;
             group_dequantize_kernel<T, S><<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>(
-                (const uint32_t *)codes, (const S *)scales, rows, cols, group, (int)groups, gq_w4_row_bytes(cols) / 4, (T *)out);
+                (const uint32_t *)codes, (const S *)scales, units, cols, (uint32_t)per_row, group == 32 ? 5 : group == 64 ? 6 : 7,
+                (int)((cols + group - 1) / group), (uint32_t)(gq_w4_row_bytes(cols) / 4), (T *)out);
             return launched();
         });
     });
