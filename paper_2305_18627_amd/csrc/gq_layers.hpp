@@ -16,42 +16,109 @@ typedef _Float16 f16;
 // A row of n columns of which eight consecutive ones are a lane's unit.  Rows may begin at any multiple of the element's size:
 // the hardware loads and stores 16 bytes at such addresses, so odd row lengths need no path of their own, only a guarded
 // last unit.
-template <typename T> struct Eight { T e[8]; };
+// Kept as words: an element a register is what becomes of them otherwise where a guarded and an unguarded load meet.
+template <typename T> struct Eight {
+    uint32_t w __attribute__((ext_vector_type(2 * sizeof(T))));
+    __device__ __forceinline__ float f(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        const uint32_t v = w[i / 2];
+        if constexpr (std::is_same<T, bf16>::value) return __uint_as_float((i & 1) ? v & 0xFFFF0000u : v << 16);
+        return (float)__builtin_bit_cast(f16, (uint16_t)((i & 1) ? v >> 16 : v));
+    }
+};
+// 16 bytes at an address that is a multiple of an element's size
+template <size_t SIZE> struct Chunk;
+template <> struct Chunk<4> { typedef uint32_t bits; typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Chunk<2> { typedef uint16_t bits; typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
 
-template <typename T> __device__ __forceinline__ void load8(const T *p, int valid, float *v)
+// t without its first `over` elements, zeros behind: by 4, 2 and 1 of them
+template <int WORDS, typename T> __device__ __forceinline__ void drop_words(Eight<T> &t, bool really)
 {
-    Eight<T> t;
-    if (valid >= 8) {
-        __builtin_memcpy(&t, p, sizeof(t));
+    constexpr int kWords = 2 * sizeof(T);
+#pragma unroll
+    for (int i = 0; i < kWords; i++) {
+        const uint32_t from = i + WORDS < kWords ? t.w[(i + WORDS) % kWords] : 0u;
+        t.w[i] = really ? from : t.w[i];
+    }
+}
+template <typename T> __device__ __forceinline__ void drop_low(Eight<T> &t, int64_t over)
+{
+    constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
+    drop_words<4 / kPer>(t, over & 4);
+    drop_words<2 / kPer>(t, over & 2);
+    if constexpr (kPer == 1) {
+        drop_words<1>(t, over & 1);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++) t.e[i] = i < valid ? p[i] : (T)0.0f;
+        for (int i = 0; i < kWords; i++) {
+            const uint32_t from = (t.w[i] >> 16) | (i + 1 < kWords ? t.w[(i + 1) % kWords] << 16 : 0u);
+            t.w[i] = (over & 1) ? from : t.w[i];
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = (float)t.e[i];
+    for (int i = 0; i < kWords; i++) t.w[i] = over < 8 ? t.w[i] : 0u;
 }
 
-template <typename T> __device__ __forceinline__ void store8(T *p, int valid, const float *v)
+// Columns c .. c + 7 of a row of n.  ask8() loads without a branch per lane: a unit that runs over the row's end (or lies past it) is
+// read so that it ends there, and settle8() moves it into place, zeros past the end.  Between the two the caller asks for more: a
+// load behind a branch would be waited for there.  ONCE: non-temporal, what no other row reads again.
+// TINY: rows of fewer than eight columns; they have kernels of their own, for this way through, with its branches and waits, slows the
+// other one down even where it is not taken.
+template <bool ONCE, bool TINY, typename T> __device__ __forceinline__ void ask8(const T *row, int64_t n, int64_t c, Eight<T> &t)
 {
-    Eight<T> t;
+    typedef typename Chunk<sizeof(T)>::type V;
+    typedef typename Chunk<sizeof(T)>::bits Bits;
+    constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
+    if (!TINY) {
+        const V *at = reinterpret_cast<const V *>(row + (c < n - 8 ? c : n - 8));
+#pragma unroll
+        for (int i = 0; i < kWords / 4; i++) {
+            const V v = ONCE ? __builtin_nontemporal_load(at + i) : at[i];
+#pragma unroll
+            for (int j = 0; j < 4; j++) t.w[4 * i + j] = v[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kWords; j++) {
+            t.w[j] = 0u;
+#pragma unroll
+            for (int i = 0; i < kPer; i++)
+                if (c + kPer * j + i < n) t.w[j] |= (uint32_t) reinterpret_cast<const Bits *>(row)[c + kPer * j + i] << (8 * sizeof(T) * i);
+        }
+    }
+}
+template <bool TINY, typename T> __device__ __forceinline__ void settle8(int64_t n, int64_t c, Eight<T> &t)
+{
+    if (!TINY && c > n - 8) drop_low(t, c - (n - 8));
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, int64_t left, const float *v)
+{
+    typedef typename Chunk<sizeof(T)>::type V;
+    struct { T e[8]; } t;
 #pragma unroll
     for (int i = 0; i < 8; i++) t.e[i] = (T)v[i];                      // to nearest even
-    if (valid >= 8) {
-        __builtin_memcpy(p, &t, sizeof(t));
+    if (left >= 8) {
+#pragma unroll
+        for (size_t i = 0; i < sizeof(t) / 16; i++) {
+            V c;
+            __builtin_memcpy(&c, reinterpret_cast<const char *>(&t) + 16 * i, 16);
+            __builtin_nontemporal_store(c, reinterpret_cast<V *>(p) + i);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (i < valid) p[i] = t.e[i];
+            if (i < left) p[i] = t.e[i];
     }
 }
 
-// Row and unit within it of a workgroup's lane, where rows have `per_row` units: one 64-bit division a workgroup, on the scalar
-// unit, and a 32-bit one a lane.
+// Row and unit within it of a lane's k-th unit, where rows have `per_row` units and a workgroup takes UNITS * kBlock of them: one
+// 64-bit division a workgroup, on the scalar unit, and a 32-bit one a unit.  The row may lie past the last one.
 struct RowUnit { int64_t row; uint32_t unit; };
-__device__ __forceinline__ RowUnit row_unit(uint32_t block, uint32_t per_row)
+template <int UNITS> __device__ __forceinline__ RowUnit row_unit(uint32_t block, int k, uint32_t per_row)
 {
-    const uint64_t first = (uint64_t)block * kBlock, row = first / per_row;
-    const uint32_t at = (uint32_t)(first - row * per_row) + threadIdx.x;           // below 2^28 + 256 for every matrix that fits
+    const uint64_t first = (uint64_t)block * (UNITS * kBlock), row = first / per_row;
+    const uint32_t at = (uint32_t)(first - row * per_row) + (uint32_t)k * kBlock + threadIdx.x;    // below 2^28 + 2^12 for a matrix that fits
     const uint32_t more = at / per_row;
     return {(int64_t)row + more, at - more * per_row};
 }

@@ -9,28 +9,46 @@
 
 namespace gq {
 
-constexpr int kNormBlock = 256;
+// A row belongs to a team of WPR waves, whose lanes hold STEPS units of eight columns each, 64 WPR units apart, from the first
+// load to the last store: a row is read once.  Teams of one wave share a workgroup of four.
+template <int WPR> constexpr int kTeams = WPR == 1 ? 4 : 1;
+template <int WPR> constexpr int kThreads = 64 * WPR * kTeams<WPR>;
 
-// the sum over a workgroup, the same for all its lanes
-__device__ __forceinline__ double block_sum(double v, double *lds)
+// the sum over a team, the same for all its lanes; `lds` is not used again before the workgroup's next barrier but one
+template <int WPR> __device__ __forceinline__ double team_sum(double v, double *lds)
 {
     v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double s = 0.0;
-    for (unsigned i = 0; i < blockDim.x / 64; i++) s += lds[i];
-    return s;
+    if constexpr (WPR == 1) {
+        return v;
+    } else {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < WPR; i++) s += lds[i];
+        return s;
+    }
 }
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds)
+template <int WPR> __device__ __forceinline__ uint32_t team_max(uint32_t v, uint32_t *lds)
 {
     v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint32_t m = 0;
-    for (unsigned i = 0; i < blockDim.x / 64; i++) m = max(m, lds[i]);
-    return m;
+    if constexpr (WPR == 1) {
+        return v;
+    } else {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < WPR; i++) m = max(m, lds[i]);
+        return m;
+    }
+}
+
+// 1 / sqrt(v) to about 2^-50: the instruction's estimate (2^-26 or better) and one step of Newton's method
+__device__ __forceinline__ float reciprocal_root(double v)
+{
+    const double y = __builtin_amdgcn_rsq(v);
+    return v <= 1e300 ? (float)(y * (1.5 - 0.5 * v * y * y)) : (float)y;      // of an infinity: 0, which the step would make a NaN
 }
 
 struct RowScale { float scale, inv; };
@@ -50,115 +68,328 @@ __device__ __forceinline__ float code_of(float y, float inv, float top)
     return inv == 0.0f ? 0.0f : __builtin_amdgcn_fmed3f(y * inv, -top, top);
 }
 
-// A workgroup per row, the row's h in LDS.
-template <typename T, typename W>
-__global__ void __launch_bounds__(kNormBlock)
-rms_norm_kernel(const T *x, const T *residual, int64_t n, const W *weight, float eps, int with_drop, Drop drop, T *sum_out, void *out,
-                int out_dtype, float *scales_out, float *rstd_out)
+struct NormArgs {
+    const void *x, *residual, *weight;
+    void *sum_out, *out;
+    float *scales_out, *rstd_out;
+    int64_t rows;
+    int n, units;                  // units of eight columns a row
+    double per_n, eps;             // 1 / n
+    int draws, out_dtype;          // random bits an element, 0: no dropout
+    Drop drop;
+};
+
+template <typename T, typename W, int WPR, int STEPS, bool TINY, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads<WPR>)
+rms_norm_kernel(NormArgs p)
 {
-    extern __shared__ float h[];
-    __shared__ double sums[kNormBlock / 64];
-    __shared__ uint32_t tops[kNormBlock / 64];
-    const int64_t row = blockIdx.x, at = row * n;
-    const int units = (int)((n + 7) / 8);
+    __shared__ double sums[WPR];
+    __shared__ uint32_t tops[WPR];
+    constexpr int kLanes = 64 * WPR;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t row = (int64_t)blockIdx.x * kTeams<WPR> + threadIdx.x / kLanes;
+    if (WPR == 1 && row >= p.rows) return;                            // whole waves; there is no barrier in them
+    const T *x = (const T *)p.x + row * p.n, *residual = (const T *)p.residual + row * p.n;
+    const W *weight = (const W *)p.weight;
+
+    Eight<T> xr[STEPS], rr[STEPS];
+    Eight<W> w[STEPS];
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        ask8<true, TINY>(x, p.n, 8 * (lane + k * kLanes), xr[k]);
+        if (RESIDUAL) ask8<true, TINY>(residual, p.n, 8 * (lane + k * kLanes), rr[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) ask8<false, TINY>(weight, p.n, 8 * (lane + k * kLanes), w[k]);
+    float h[STEPS][8];
     double ss = 0.0;
-    for (int u = threadIdx.x; u < units; u += kNormBlock) {
-        const int valid = (int)(n - 8 * u < 8 ? n - 8 * u : 8);
-        float v[8];
-        load8(x + at + 8 * u, valid, v);
-        if (with_drop == 32) drop8<false>(drop, drop.first + 8 * ((uint64_t)row * units + u), v);
-        if (with_drop == 16) drop8<true>(drop, drop.first + 8 * ((uint64_t)row * units + u), v);
-        if (residual) {
-            float r[8];
-            load8(residual + at + 8 * u, valid, r);
-            for (int i = 0; i < 8; i++) v[i] = r[i] + v[i];
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        const int u = lane + k * kLanes;
+        settle8<TINY>(p.n, 8 * u, xr[k]);
+        if (RESIDUAL) settle8<TINY>(p.n, 8 * u, rr[k]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) h[k][i] = xr[k].f(i);
+        const uint64_t g = p.drop.first + 8 * ((uint64_t)row * p.units + u);
+        if (p.draws == 32) drop8<false>(p.drop, g, h[k]);
+        if (p.draws == 16) drop8<true>(p.drop, g, h[k]);
+        if (RESIDUAL) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) h[k][i] = rr[k].f(i) + h[k][i];
         }
-        if (sum_out) store8(sum_out + at + 8 * u, valid, v);
-        for (int i = 0; i < 8; i++) {
-            h[8 * u + i] = v[i];
-            ss += (double)v[i] * (double)v[i];
-        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) ss = __builtin_fma((double)h[k][i], (double)h[k][i], ss);    // zeros past the row's end
     }
-    ss = block_sum(ss, sums);
-    const float rstd = (float)(1.0 / sqrt(ss / (double)n + (double)eps));
-    if (rstd_out && threadIdx.x == 0) rstd_out[row] = rstd;
-    RowScale rs = {1.0f, 1.0f};
-    const float top = out_dtype == GQ_I8 ? 127.0f : 448.0f;
-    if (scales_out) {
-        uint32_t m = 0;
-        for (int u = threadIdx.x; u < units; u += kNormBlock)
-            for (int i = 0; i < 8; i++)
-                if (8 * u + i < n) m = max(m, __float_as_uint((h[8 * u + i] * rstd) * (float)weight[8 * u + i]) & 0x7FFFFFFFu);
-        rs = row_scale(block_max(m, tops), top);
-        if (threadIdx.x == 0) scales_out[row] = rs.scale;
+    ss = team_sum<WPR>(ss, sums);
+    const float rstd = reciprocal_root(__builtin_fma(ss, p.per_n, p.eps));
+    if (p.rstd_out && lane == 0) p.rstd_out[row] = rstd;
+    if (p.sum_out) {
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) store8((T *)p.sum_out + row * p.n + 8 * (lane + k * kLanes), p.n - 8 * (lane + k * kLanes), h[k]);
     }
-    for (int u = threadIdx.x; u < units; u += kNormBlock) {
-        const int valid = (int)(n - 8 * u < 8 ? n - 8 * u : 8);
-        float v[8];
-        for (int i = 0; i < 8; i++) v[i] = i < valid ? (h[8 * u + i] * rstd) * (float)weight[8 * u + i] : 0.0f;
-        if (!scales_out) {
-            store8((T *)out + at + 8 * u, valid, v);
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        settle8<TINY>(p.n, 8 * (lane + k * kLanes), w[k]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) h[k][i] = (h[k][i] * rstd) * w[k].f(i);
+    }
+    if (!p.scales_out) {
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) store8((T *)p.out + row * p.n + 8 * (lane + k * kLanes), p.n - 8 * (lane + k * kLanes), h[k]);
+        return;
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < STEPS; k++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, 8 * (lane + k * kLanes) + i < p.n ? __float_as_uint(h[k][i]) & 0x7FFFFFFFu : 0u);
+    const float top = p.out_dtype == GQ_I8 ? 127.0f : 448.0f;
+    const RowScale rs = row_scale(team_max<WPR>(m, tops), top);
+    if (lane == 0) p.scales_out[row] = rs.scale;
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        float c[8];
+        struct { uint8_t e[8]; } o;
+#pragma unroll
+        for (int i = 0; i < 8; i++) c[i] = code_of(h[k][i], rs.inv, top);
+        if (p.out_dtype == GQ_I8) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) o.e[i] = (uint8_t)(int8_t)(int)__builtin_rintf(c[i]);
         } else {
-            for (int i = 0; i < valid; i++) {
-                const float c = code_of(v[i], rs.inv, top);
-                if (out_dtype == GQ_I8) ((int8_t *)out)[at + 8 * u + i] = (int8_t)__builtin_rintf(c);
-                else ((uint8_t *)out)[at + 8 * u + i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false);
+            u32x2 v = {0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                v[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i], c[4 * i + 1], 0, false);
+                v[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i + 2], c[4 * i + 3], (int)v[i], true);
             }
+            __builtin_memcpy(&o, &v, 8);
+        }
+        const int u = lane + k * kLanes, left = p.n - 8 * u;
+        uint8_t *at = (uint8_t *)p.out + row * p.n + 8 * u;
+        if (left >= 8) {
+            __builtin_memcpy(at, &o, 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (i < left) at[i] = o.e[i];
         }
     }
 }
 
+struct BackwardArgs {
+    const void *dy, *h, *dsum, *weight;
+    const float *rstd;
+    void *dres_out, *dx_out;
+    float *parts;                  // [teams' workgroups][8 units], or NULL
+    int64_t rows;
+    int n, units;
+    double per_n;
+    int draws;
+    Drop drop;
+};
+
+// the compiler may not keep what it computed from these before
+template <typename T> __device__ __forceinline__ void forget(Eight<T> &t)
+{
+#pragma unroll
+    for (size_t i = 0; i < sizeof(t) / 4; i++) {
+        uint32_t w = t.w[i];
+        asm volatile("" : "+v"(w));
+        t.w[i] = w;
+    }
+}
+
+// A workgroup takes rows (its teams one each) in turn, gridDim.x * teams apart, and keeps the weight's gradient of its columns in
+// registers; its sums go to `parts` and a second kernel adds those up.  AHEAD: the next row is asked for before the current one is
+// reduced, where the registers reach.
+template <typename T, typename W, int WPR, int STEPS, bool TINY, bool DSUM, bool AHEAD>
+__global__ void __launch_bounds__(kThreads<WPR>)
+rms_norm_backward_kernel(BackwardArgs p)
+{
+    constexpr int kLanes = 64 * WPR, kTeam = kTeams<WPR>;
+    __shared__ double sums[2][WPR];
+    __shared__ float joined[kTeam > 1 ? kTeam - 1 : 1][kTeam > 1 ? STEPS * 512 : 1];
+    const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
+    const int64_t stride = (int64_t)gridDim.x * kTeam;
+    struct Row { Eight<T> dy[STEPS], h[STEPS], ds[DSUM ? STEPS : 1]; float rstd; };
+    auto fetch = [&](int64_t row, Row &r) {
+        r.rstd = p.rstd[row];
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) {
+            const int c = 8 * (lane + k * kLanes);
+            ask8<true, TINY>((const T *)p.dy + row * p.n, p.n, c, r.dy[k]);
+            ask8<true, TINY>((const T *)p.h + row * p.n, p.n, c, r.h[k]);
+            if (DSUM) ask8<true, TINY>((const T *)p.dsum + row * p.n, p.n, c, r.ds[k]);
+        }
+    };
+    Eight<W> w[STEPS];
+    Row now, next;
+    float dw[STEPS][8];
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        ask8<false, TINY>((const W *)p.weight, p.n, 8 * (lane + k * kLanes), w[k]);
+        settle8<TINY>(p.n, 8 * (lane + k * kLanes), w[k]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dw[k][i] = 0.0f;
+    }
+    int64_t row = (int64_t)blockIdx.x * kTeam + team;
+    if (AHEAD && row < p.rows) fetch(row, now);
+    for (int turn = 0; row < p.rows; row += stride, turn ^= 1) {
+        if (!AHEAD) fetch(row, now);
+        if (AHEAD && row + stride < p.rows) fetch(row + stride, next);
+        const float rstd = now.rstd;
+        double s = 0.0;
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) {
+            settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.dy[k]);
+            settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.h[k]);
+            if (DSUM) settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.ds[k]);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float dy = now.dy[k].f(i), xh = now.h[k].f(i) * rstd;
+                s = __builtin_fma((double)(dy * w[k].f(i)), (double)xh, s);
+                dw[k][i] += dy * xh;
+            }
+            __builtin_amdgcn_sched_barrier(0);                        // a unit after another: all at once hold too many registers
+        }
+        const float mean = (float)(team_sum<WPR>(s, sums[turn]) * p.per_n);
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) {
+            const int u = lane + k * kLanes, left = p.n - 8 * u;
+            const int64_t at = row * p.n + 8 * u;
+            forget(now.dy[k]);
+            forget(now.h[k]);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float g = now.dy[k].f(i) * w[k].f(i), xh = now.h[k].f(i) * rstd;
+                v[i] = rstd * (g - xh * mean);
+                if (DSUM) v[i] = now.ds[k].f(i) + v[i];
+            }
+            if (p.dres_out) store8((T *)p.dres_out + at, left, v);
+            const uint64_t g = p.drop.first + 8 * ((uint64_t)row * p.units + u);
+            if (p.draws == 32) drop8<false>(p.drop, g, v);
+            if (p.draws == 16) drop8<true>(p.drop, g, v);
+            store8((T *)p.dx_out + at, left, v);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (AHEAD) now = next;
+    }
+    if (!p.parts) return;
+    if (kTeam > 1) {
+        if (team > 0) {
+#pragma unroll
+            for (int k = 0; k < STEPS; k++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) joined[team - 1][(k * 8 + i) * 64 + lane] = dw[k][i];
+        }
+        __syncthreads();
+        if (team > 0) return;
+#pragma unroll
+        for (int t = 0; t < kTeam - 1; t++)
+#pragma unroll
+            for (int k = 0; k < STEPS; k++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) dw[k][i] += joined[t][(k * 8 + i) * 64 + lane];
+    }
+    float *part = p.parts + (int64_t)blockIdx.x * p.units * 8;
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        const int u = lane + k * kLanes;
+        if (u < p.units) {
+            *reinterpret_cast<f32x4 *>(part + 8 * u) = f32x4{dw[k][0], dw[k][1], dw[k][2], dw[k][3]};
+            *reinterpret_cast<f32x4 *>(part + 8 * u + 4) = f32x4{dw[k][4], dw[k][5], dw[k][6], dw[k][7]};
+        }
+    }
+}
+
+// The same for rows that the registers of a team do not hold: each is read twice, the weight's gradient is kept in LDS.
+constexpr int kLongBlock = 1024;
 template <typename T, typename W>
-__global__ void __launch_bounds__(kNormBlock)
-rms_norm_backward_kernel(const T *dy, const T *h, const T *dsum, int64_t n, const W *weight, const float *rstds, int with_drop,
-                         Drop drop, T *dres_out, T *dx_out)
+__global__ void __launch_bounds__(kLongBlock)
+rms_norm_backward_long_kernel(BackwardArgs p)
 {
-    __shared__ double sums[kNormBlock / 64];
-    const int64_t row = blockIdx.x, at = row * n;
-    const int units = (int)((n + 7) / 8);
-    const float rstd = rstds[row];
-    double s = 0.0;
-    for (int64_t c = threadIdx.x; c < n; c += kNormBlock) s += (double)((float)dy[at + c] * (float)weight[c]) * (double)((float)h[at + c] * rstd);
-    const float mean = (float)(block_sum(s, sums) / (double)n);
-    for (int u = threadIdx.x; u < units; u += kNormBlock) {
-        const int valid = (int)(n - 8 * u < 8 ? n - 8 * u : 8);
-        float v[8], a[8], b[8];
-        load8(dy + at + 8 * u, valid, a);
-        load8(h + at + 8 * u, valid, b);
-        for (int i = 0; i < 8; i++) v[i] = rstd * (a[i] * (i < valid ? (float)weight[8 * u + i] : 0.0f) - (b[i] * rstd) * mean);
-        if (dsum) {
-            load8(dsum + at + 8 * u, valid, a);
-            for (int i = 0; i < 8; i++) v[i] = a[i] + v[i];
+    constexpr int kWaves = kLongBlock / 64;
+    extern __shared__ f32x4 dw[];                                     // [units][2], each touched by one lane only
+    __shared__ double sums[2][kWaves];
+    for (int u = threadIdx.x; u < p.units; u += kLongBlock) dw[2 * u] = dw[2 * u + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        const float rstd = p.rstd[row];
+        const T *dy = (const T *)p.dy + row * p.n, *h = (const T *)p.h + row * p.n;
+        double s = 0.0;
+        for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
+            Eight<T> a, b;
+            Eight<W> w;
+            ask8<false, false>(dy, p.n, 8 * u, a);
+            ask8<false, false>(h, p.n, 8 * u, b);
+            ask8<false, false>((const W *)p.weight, p.n, 8 * u, w);
+            settle8<false>(p.n, 8 * u, a);
+            settle8<false>(p.n, 8 * u, b);
+            settle8<false>(p.n, 8 * u, w);
+            f32x4 d[2] = {dw[2 * u], dw[2 * u + 1]};
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float xh = b.f(i) * rstd;
+                s = __builtin_fma((double)(a.f(i) * w.f(i)), (double)xh, s);
+                d[i / 4][i % 4] += a.f(i) * xh;
+            }
+            dw[2 * u] = d[0];
+            dw[2 * u + 1] = d[1];
         }
-        if (dres_out) store8(dres_out + at + 8 * u, valid, v);
-        if (with_drop == 32) drop8<false>(drop, drop.first + 8 * ((uint64_t)row * units + u), v);
-        if (with_drop == 16) drop8<true>(drop, drop.first + 8 * ((uint64_t)row * units + u), v);
-        store8(dx_out + at + 8 * u, valid, v);
+        const float mean = (float)(team_sum<kWaves>(s, sums[turn]) * p.per_n);
+        for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
+            const int left = p.n - 8 * u;
+            Eight<T> a, b, c;
+            Eight<W> w;
+            ask8<true, false>(dy, p.n, 8 * u, a);
+            ask8<true, false>(h, p.n, 8 * u, b);
+            ask8<false, false>((const W *)p.weight, p.n, 8 * u, w);
+            if (p.dsum) ask8<true, false>((const T *)p.dsum + row * p.n, p.n, 8 * u, c);
+            settle8<false>(p.n, 8 * u, a);
+            settle8<false>(p.n, 8 * u, b);
+            settle8<false>(p.n, 8 * u, w);
+            if (p.dsum) settle8<false>(p.n, 8 * u, c);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                v[i] = rstd * (a.f(i) * w.f(i) - (b.f(i) * rstd) * mean);
+                if (p.dsum) v[i] = c.f(i) + v[i];
+            }
+            if (p.dres_out) store8((T *)p.dres_out + row * p.n + 8 * u, left, v);
+            const uint64_t g = p.drop.first + 8 * ((uint64_t)row * p.units + u);
+            if (p.draws == 32) drop8<false>(p.drop, g, v);
+            if (p.draws == 16) drop8<true>(p.drop, g, v);
+            store8((T *)p.dx_out + row * p.n + 8 * u, left, v);
+        }
+    }
+    if (!p.parts) return;
+    f32x4 *part = reinterpret_cast<f32x4 *>(p.parts + (int64_t)blockIdx.x * p.units * 8);
+    for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
+        part[2 * u] = dw[2 * u];
+        part[2 * u + 1] = dw[2 * u + 1];
     }
 }
 
-constexpr int kWeightParts = 256;      // stretches of rows whose sums are added up by a second kernel
-
-template <typename T>
-__global__ void __launch_bounds__(kNormBlock)
-weight_partial_kernel(const T *dy, const T *h, int64_t rows, int64_t n, const float *rstds, float *parts)
+// A workgroup adds up `count` parts of 64 columns: 16 lanes of four columns, 16 slices of the parts, joined in a fixed order.
+__global__ void __launch_bounds__(256)
+weight_sum_kernel(const float *parts, int count, int n, int pitch, float *dweight)
 {
-    const int64_t c = (int64_t)blockIdx.x * kNormBlock + threadIdx.x;
-    if (c >= n) return;
-    const int64_t per = (rows + gridDim.y - 1) / gridDim.y, first = per * blockIdx.y, last = first + per < rows ? first + per : rows;
-    float s = 0.0f;
-    for (int64_t r = first; r < last; r++) s += (float)dy[r * n + c] * ((float)h[r * n + c] * rstds[r]);
-    parts[(int64_t)blockIdx.y * n + c] = s;
-}
-
-__global__ void __launch_bounds__(kNormBlock)
-weight_sum_kernel(const float *parts, int count, int64_t n, float *dweight)
-{
-    const int64_t c = (int64_t)blockIdx.x * kNormBlock + threadIdx.x;
-    if (c >= n) return;
-    float s = 0.0f;
-    for (int i = 0; i < count; i++) s += parts[(int64_t)i * n + c];
-    dweight[c] = s;
+    __shared__ f32x4 slices[16][16];
+    const int c4 = threadIdx.x % 16, slice = threadIdx.x / 16, c = blockIdx.x * 64 + 4 * c4;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < pitch) {
+#pragma unroll 8
+        for (int i = slice; i < count; i += 16) s += *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * pitch + c);
+    }
+    slices[slice][c4] = s;
+    __syncthreads();
+    const int column = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || column >= n) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t += slices[i][threadIdx.x / 4][threadIdx.x % 4];
+    dweight[column] = t;
 }
 
 static gq_status check_norm(int64_t rows, int64_t n, int dtype, int weight_dtype, const gq_dropout_params *drop)
@@ -177,7 +408,28 @@ template <typename F> static gq_status with_types(int dtype, int weight_dtype, F
     });
 }
 
-static int64_t weight_parts(int64_t rows) { return rows < kWeightParts ? (rows > 0 ? rows : 1) : kWeightParts; }
+// f(waves per row, steps, fewer than eight columns) of the smallest team that holds a row of n columns, as compile-time constants
+template <typename F> static gq_status with_team(int64_t n, F &&f)
+{
+    using std::integral_constant;
+    const std::false_type no;
+    if (n < 8) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), std::true_type());
+    if (n <= 512) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), no);
+    if (n <= 1024) return f(integral_constant<int, 1>(), integral_constant<int, 2>(), no);
+    if (n <= 2048) return f(integral_constant<int, 4>(), integral_constant<int, 1>(), no);
+    if (n <= 4096) return f(integral_constant<int, 4>(), integral_constant<int, 2>(), no);
+    if (n <= 6144) return f(integral_constant<int, 4>(), integral_constant<int, 3>(), no);
+    if (n <= 8192) return f(integral_constant<int, 4>(), integral_constant<int, 4>(), no);
+    if (n <= 16384) return f(integral_constant<int, 16>(), integral_constant<int, 2>(), no);
+    return f(integral_constant<int, 16>(), integral_constant<int, 4>(), no);
+}
+
+// workgroups of the backward pass, each of which leaves one part of the weight's gradient
+static int64_t backward_groups(int64_t rows, int64_t n)
+{
+    const int64_t teams = n <= 1024 ? (rows + 3) / 4 : rows, most = n <= 8192 ? 512 : 256;
+    return teams < 1 ? 1 : teams < most ? teams : most;
+}
 
 }  // namespace gq
 
@@ -196,24 +448,27 @@ gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t
     if (rows == 0 || n == 0) return GQ_OK;
     if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(out, 16) || !aligned_or_null(residual, 16) || !aligned_or_null(sum_out, 16) ||
         !aligned_or_null(scales_out, 4) || !aligned_or_null(rstd_out, 4) || out == sum_out) return GQ_ERR_INVALID_ARG;
-    if (!grid_fits(rows, kNormBlock)) return GQ_ERR_INVALID_ARG;
-    const Drop d = drop ? make_drop(drop) : Drop{};
+    const NormArgs p = {x, residual, weight, sum_out, out, scales_out, rstd_out, rows, (int)n, (int)(pitch8(n) / 8), 1.0 / (double)n, (double)eps,
+                        draw_bits(drop), (int)out_dtype, drop ? make_drop(drop) : Drop{}};
     return with_types(dtype, weight_dtype, [&](auto t, auto w) {
         typedef decltype(t) T;
         typedef decltype(w) W;
-        const unsigned lds = (unsigned)(4 * pitch8(n));
-        auto kernel = rms_norm_kernel<T, W>;
-        if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return GQ_ERR_DEVICE;
-        kernel<<<(unsigned)rows, kNormBlock, lds, (hipStream_t)hip_stream>>>(
-            (const T *)x, (const T *)residual, n, (const W *)weight, eps, draw_bits(drop), d, (T *)sum_out, out, out_dtype, scales_out, rstd_out);
-        return launched();
+        return with_team(n, [&](auto wpr, auto steps, auto tiny) {
+            constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value;
+            constexpr bool TINY = decltype(tiny)::value;
+            const int64_t blocks = (rows + kTeams<WPR> - 1) / kTeams<WPR>;
+            if (!grid_fits(blocks, kThreads<WPR>)) return GQ_ERR_INVALID_ARG;
+            auto kernel = residual ? rms_norm_kernel<T, W, WPR, STEPS, TINY, true> : rms_norm_kernel<T, W, WPR, STEPS, TINY, false>;
+            kernel<<<(unsigned)blocks, kThreads<WPR>, 0, (hipStream_t)hip_stream>>>(p);
+            return launched();
+        });
     });
 }
 
 size_t gq_rms_norm_workspace_bytes(int64_t rows, int64_t n)
 {
     if (!matrix_fits(rows, n) || n > GQ_RMS_NORM_MAX_N) return 0;
-    return (size_t)(weight_parts(rows) * pitch8(n) * 4);
+    return (size_t)(backward_groups(rows, n) * pitch8(n) * 4);
 }
 
 gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, int64_t rows, int64_t n, gq_dtype dtype,
@@ -226,24 +481,35 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
     if (n == 0 || (rows == 0 && !dweight_out)) return GQ_OK;
     if (rows > 0 && (!aligned(dy, 16) || !aligned(h, 16) || !aligned(weight, 16) || !aligned(rstd, 4) || !aligned(dx_out, 16) ||
                      !aligned_or_null(dsum, 16) || !aligned_or_null(dres_out, 16) || dres_out == dx_out)) return GQ_ERR_INVALID_ARG;
-    if (!aligned_or_null(dweight_out, 16) || !grid_fits(rows, kNormBlock)) return GQ_ERR_INVALID_ARG;
+    if (!aligned_or_null(dweight_out, 16)) return GQ_ERR_INVALID_ARG;
     if (dweight_out && (!aligned(workspace, 16) || workspace_bytes < gq_rms_norm_workspace_bytes(rows, n))) return GQ_ERR_WORKSPACE;
-    const Drop d = drop ? make_drop(drop) : Drop{};
-    return with_types(dtype, weight_dtype, [&](auto t, auto w) {
-        typedef decltype(t) T;
-        typedef decltype(w) W;
-        const hipStream_t stream = (hipStream_t)hip_stream;
-        if (dweight_out) {                                             // before dx: dx_out may be dy
-            const unsigned cols = (unsigned)((n + kNormBlock - 1) / kNormBlock);
-            const int parts = (int)weight_parts(rows);
-            weight_partial_kernel<T><<<dim3(cols, parts), kNormBlock, 0, stream>>>((const T *)dy, (const T *)h, rows, n, rstd, (float *)workspace);
-            weight_sum_kernel<<<cols, kNormBlock, 0, stream>>>((const float *)workspace, parts, n, dweight_out);
-        }
-        if (rows > 0)
-            rms_norm_backward_kernel<T, W><<<(unsigned)rows, kNormBlock, 0, stream>>>((const T *)dy, (const T *)h, (const T *)dsum, n, (const W *)weight, rstd,
-                                                                                     draw_bits(drop), d, (T *)dres_out, (T *)dx_out);
-        return launched();
-    });
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t groups = backward_groups(rows, n);
+    const BackwardArgs p = {dy, h, dsum, weight, rstd, dres_out, dx_out, dweight_out ? (float *)workspace : nullptr, rows, (int)n,
+                            (int)(pitch8(n) / 8), 1.0 / (double)n, draw_bits(drop), drop ? make_drop(drop) : Drop{}};
+    if (rows > 0) {
+        const gq_status launch = with_types(dtype, weight_dtype, [&](auto t, auto w) {
+            typedef decltype(t) T;
+            typedef decltype(w) W;
+            return with_team(n, [&](auto wpr, auto steps, auto tiny) {
+                constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value;
+                constexpr bool TINY = decltype(tiny)::value;
+                if constexpr (WPR * STEPS >= 64) {
+                    rms_norm_backward_long_kernel<T, W><<<(unsigned)groups, kLongBlock, 32 * (unsigned)p.units, stream>>>(p);
+                } else {
+                    constexpr bool kAhead = WPR < 16 && STEPS * sizeof(T) <= 4;
+                    auto kernel = dsum ? rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, true, kAhead>
+                                       : rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, false, kAhead>;
+                    kernel<<<(unsigned)groups, kThreads<WPR>, 0, stream>>>(p);
+                }
+                return launched();
+            });
+        });
+        if (launch != GQ_OK) return launch;
+    }
+    if (!dweight_out) return GQ_OK;
+    weight_sum_kernel<<<(unsigned)((n + 63) / 64), 256, 0, stream>>>((const float *)workspace, rows > 0 ? (int)groups : 0, (int)n, (int)pitch8(n), dweight_out);
+    return launched();
 }
 
 }  // extern "C"
