@@ -424,10 +424,30 @@ template <typename F> static gq_status with_team(int64_t n, F &&f)
     return f(integral_constant<int, 16>(), integral_constant<int, 4>(), no);
 }
 
-// workgroups of the backward pass, each of which leaves one part of the weight's gradient
-static int64_t backward_groups(int64_t rows, int64_t n)
+// The same for the backward pass, whose rows come with twice the registers; none for rows of more than 16384 columns.
+template <typename F> static gq_status with_backward_team(int64_t n, F &&f)
 {
-    const int64_t teams = n <= 1024 ? (rows + 3) / 4 : rows, most = n <= 8192 ? 512 : 256;
+    using std::integral_constant;
+    const std::false_type no;
+    if (n < 8) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), std::true_type());
+    if (n <= 512) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), no);
+    if (n <= 1024) return f(integral_constant<int, 1>(), integral_constant<int, 2>(), no);
+    if (n <= 2048) return f(integral_constant<int, 4>(), integral_constant<int, 1>(), no);
+    if (n <= 4096) return f(integral_constant<int, 8>(), integral_constant<int, 1>(), no);
+    if (n <= 6144) return f(integral_constant<int, 12>(), integral_constant<int, 1>(), no);
+    if (n <= 8192) return f(integral_constant<int, 8>(), integral_constant<int, 2>(), no);
+    return f(integral_constant<int, 16>(), integral_constant<int, 2>(), no);
+}
+
+// Workgroups of the backward pass, each of which leaves one part of the weight's gradient: one a compute unit where it has enough
+// waves of its own and asks ahead, else two.  bf16, us with 256 and 512: 8192x4096 47.8 and 51.8, with dropout (more arithmetic, and
+// no asking ahead) 74.6 and 64.3; 16384x2048 63.0 and 49.0, but 1000x2047 fp32 11.3 and 12.0: too few rows each to make up for the parts.
+constexpr int64_t kMostParts = 512;
+static int64_t backward_groups(int64_t rows, int64_t n, bool drop)
+{
+    const int64_t teams = n <= 1024 ? (rows + 3) / 4 : rows;
+    const bool small = n <= 512 || (n > 1024 && n <= 2048), two = n <= 16384 && (drop || small) && teams >= 4 * kMostParts;
+    const int64_t most = two ? kMostParts : kMostParts / 2;
     return teams < 1 ? 1 : teams < most ? teams : most;
 }
 
@@ -468,7 +488,7 @@ gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t
 size_t gq_rms_norm_workspace_bytes(int64_t rows, int64_t n)
 {
     if (!matrix_fits(rows, n) || n > GQ_RMS_NORM_MAX_N) return 0;
-    return (size_t)(backward_groups(rows, n) * pitch8(n) * 4);
+    return (size_t)((rows < 1 ? 1 : rows < kMostParts ? rows : kMostParts) * pitch8(n) * 4);
 }
 
 gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, int64_t rows, int64_t n, gq_dtype dtype,
@@ -484,24 +504,26 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
     if (!aligned_or_null(dweight_out, 16)) return GQ_ERR_INVALID_ARG;
     if (dweight_out && (!aligned(workspace, 16) || workspace_bytes < gq_rms_norm_workspace_bytes(rows, n))) return GQ_ERR_WORKSPACE;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const int64_t groups = backward_groups(rows, n);
+    const int64_t groups = backward_groups(rows, n, drop != nullptr);
     const BackwardArgs p = {dy, h, dsum, weight, rstd, dres_out, dx_out, dweight_out ? (float *)workspace : nullptr, rows, (int)n,
                             (int)(pitch8(n) / 8), 1.0 / (double)n, draw_bits(drop), drop ? make_drop(drop) : Drop{}};
     if (rows > 0) {
         const gq_status launch = with_types(dtype, weight_dtype, [&](auto t, auto w) {
             typedef decltype(t) T;
             typedef decltype(w) W;
-            return with_team(n, [&](auto wpr, auto steps, auto tiny) {
+            if (n > 16384) {
+                rms_norm_backward_long_kernel<T, W><<<(unsigned)groups, kLongBlock, 32 * (unsigned)p.units, stream>>>(p);
+                return launched();
+            }
+            return with_backward_team(n, [&](auto wpr, auto steps, auto tiny) {
                 constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value;
-                constexpr bool TINY = decltype(tiny)::value;
-                if constexpr (WPR * STEPS >= 64) {
-                    rms_norm_backward_long_kernel<T, W><<<(unsigned)groups, kLongBlock, 32 * (unsigned)p.units, stream>>>(p);
-                } else {
-                    constexpr bool kAhead = WPR < 16 && STEPS * sizeof(T) <= 4;
-                    auto kernel = dsum ? rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, true, kAhead>
-                                       : rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, false, kAhead>;
-                    kernel<<<(unsigned)groups, kThreads<WPR>, 0, stream>>>(p);
-                }
+                constexpr bool TINY = decltype(tiny)::value, kAhead = WPR < 16;      // as far as the registers reach
+                auto with_dsum = [&](auto there) {
+                    constexpr bool DSUM = decltype(there)::value;
+                    return groups == kMostParts && drop ? rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, DSUM, false> : rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, DSUM, kAhead>;
+                };
+                auto kernel = dsum ? with_dsum(std::true_type()) : with_dsum(std::false_type());
+                kernel<<<(unsigned)groups, kThreads<WPR>, 0, stream>>>(p);
                 return launched();
             });
         });
