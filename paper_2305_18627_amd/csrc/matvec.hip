@@ -162,49 +162,56 @@ w4_matvec_kernel(MatvecArgs p)
     }
     constexpr int kTileBytes = 16 * kStep * (int)sizeof(X);                        // of 16 rows of x, streamed
 
-    // ---- codes and scales of a step: 16 bytes a lane and chunk ----
-    struct Fetched { u32x4 w[U][RT]; float s[U][RT][kGroups]; };
+    // ---- codes and scales of a step: 16 bytes of codes a lane and chunk, the scales of its row's chunks in one load ----
+    // Both stay as they lie in memory until they are used: a conversion here would be waited for here.
+    constexpr int kScales = U * kGroups, kScaleWords = (kScales * (int)sizeof(S) + 3) / 4;
+    struct Fetched { u32x4 w[U][RT]; uint32_t s[RT][kScaleWords]; };
     const uint32_t scale_bytes = (uint32_t)(p.groups * (int)sizeof(S));
+    const int last_block = (p.cols - 1) / 32;
+    // the first scale of a step's load: where the step runs over the row's end, so early that the load does not
+    auto first_scale = [&](int step) { return min((step * WK + wk) * kScales, max(p.groups - kScales, 0)); };
     auto fetch = [&](int tile, int step, Fetched &f) {
-        // a wave whose rows all lie past the last one reads that one
+        // The wave's first row is the same for all lanes, what differs is a lane's row within the tile.  A wave whose rows all lie past
+        // the last one reads that one, and so do rows past it: never stored.
         const int first = min((tile * WN + wn) * RT * 16, p.rows - 1), c = (step * WK + wk) * U * 128;
-        // the wave's first row and column are the same for all lanes; what differs is a lane's row within the tile.  Rows past
-        // the last one: its codes again, never stored
-        const uint8_t *codes = p.codes + (int64_t)first * p.row_bytes + c / 2;
-        const uint8_t *scales = (const uint8_t *)p.scales + ((int64_t)first * p.groups + c / GROUP) * (int)sizeof(S);
+        const uint8_t *codes = p.codes + (int64_t)first * p.row_bytes;
+        const uint8_t *scales = (const uint8_t *)p.scales + ((int64_t)first * p.groups + first_scale(step)) * (int)sizeof(S);
         const int last = p.rows - 1 - first;
-        if (RESIDENT && c + U * 128 <= p.cols) {
 #pragma unroll
-            for (int t = 0; t < RT; t++) {
-                const uint32_t r = (uint32_t)min(16 * t + i16, last);
-                const uint32_t at = r * (uint32_t)p.row_bytes + 16u * (uint32_t)q;
+        for (int t = 0; t < RT; t++) {
+            const uint32_t r = (uint32_t)min(16 * t + i16, last), at = r * (uint32_t)p.row_bytes;
+            // past the row's end the last codes again, where x is zero
 #pragma unroll
-                for (int u = 0; u < U; u++) f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + at + 64 * u);
-                struct { S e[U * kGroups]; } s;
-                __builtin_memcpy(&s, scales + r * scale_bytes, sizeof(s));
+            for (int u = 0; u < U; u++)
+                f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (at + 16u * (uint32_t)min(c / 32 + 4 * u + q, last_block)));
+            if (p.groups >= kScales) {
+                if constexpr (kScaleWords * 4 != kScales * (int)sizeof(S)) f.s[t][kScaleWords - 1] = 0;
+                __builtin_memcpy(f.s[t], scales + r * scale_bytes, kScales * sizeof(S));
+            } else {                                                               // few columns
+                typedef typename std::conditional<sizeof(S) == 4, uint32_t, uint16_t>::type Bits;
+                constexpr int kPer = 4 / (int)sizeof(S);
+                const Bits *from_row = reinterpret_cast<const Bits *>(scales + r * scale_bytes);
 #pragma unroll
-                for (int u = 0; u < U; u++)
+                for (int j = 0; j < kScaleWords; j++) {
+                    f.s[t][j] = 0;
 #pragma unroll
-                    for (int g = 0; g < kGroups; g++) f.s[u][t][g] = (float)s.e[u * kGroups + g];
-            }
-        } else {
-            // past the row's end the last codes again, where x is zero, and scales of zero.  Streamed, all steps come here: a second
-            // way through costs more registers than this
-#pragma unroll
-            for (int t = 0; t < RT; t++) {
-                const uint32_t r = (uint32_t)min(16 * t + i16, last);
-#pragma unroll
-                for (int u = 0; u < U; u++) {
-                    const int b = min(c / 32 + 4 * u + q, (p.cols - 1) / 32) - c / 32;
-                    f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (int)(r * (uint32_t)p.row_bytes) + 16 * b);
-#pragma unroll
-                    for (int g = 0; g < kGroups; g++) {
-                        const int at = min(c / GROUP + u * kGroups + g, p.groups - 1) - c / GROUP;
-                        const float s = (float)*reinterpret_cast<const S *>(scales + at * (int)sizeof(S) + r * scale_bytes);
-                        f.s[u][t][g] = c / GROUP + u * kGroups + g < p.groups ? s : 0.0f;
-                    }
+                    for (int i = 0; i < kPer; i++)
+                        if (j * kPer + i < p.groups) f.s[t][j] |= (uint32_t)from_row[j * kPer + i] << (16 * i);
                 }
             }
+        }
+    };
+    // a step's scales as numbers, zeros behind the row's end
+    auto scales_of = [&](const uint32_t *words, int step, float *s) {
+#pragma unroll
+        for (int k = 0; k < kScales; k++) {
+            if constexpr (sizeof(S) == 4) s[k] = __uint_as_float(words[k]);
+            else s[k] = __uint_as_float((k & 1) ? words[k / 2] & 0xFFFF0000u : words[k / 2] << 16);
+        }
+        // what the load began too early, or what lies behind the row's end where it could not begin earlier
+        for (int late = min((step * WK + wk) * kScales - first_scale(step), kScales); late > 0; late--) {
+#pragma unroll
+            for (int k = 0; k < kScales; k++) s[k] = k + 1 < kScales ? s[k + 1] : 0.0f;
         }
     };
 
@@ -216,7 +223,10 @@ w4_matvec_kernel(MatvecArgs p)
             for (int t = 0; t < RT; t++) acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     };
     // a step's products; `staged`: where its first column is
-    auto multiply = [&](const Fetched &f, const uint8_t *staged) {
+    auto multiply = [&](const Fetched &f, int step, const uint8_t *staged) {
+        float scale[RT][kScales];
+#pragma unroll
+        for (int t = 0; t < RT; t++) scales_of(f.s[t], step, scale[t]);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const uint8_t *chunk = staged + (wk * U + u) * 16 * kUnit;
@@ -252,7 +262,7 @@ w4_matvec_kernel(MatvecArgs p)
 #pragma unroll
                         for (int j = 0; j < kBlocks; j++) s = A::product(a[i][j], b[j], s);
 #pragma unroll
-                        for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], f.s[u][t][g], acc[i][t][r]);
+                        for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], scale[t][u * kGroups + g], acc[i][t][r]);
                     }
                 }
                 // the groups one after another, sums and all: left to itself the compiler moves all sums behind all products, and
@@ -319,7 +329,7 @@ w4_matvec_kernel(MatvecArgs p)
             for (int step = 0; step < steps; step++) {
                 const bool more = step + 1 < steps;
                 if (more || tile + (int)gridDim.x < tiles) fetch(more ? tile : tile + gridDim.x, more ? step + 1 : 0, next);
-                multiply(now, lds + step * (kStep / 8) * kUnit);
+                multiply(now, step, lds + step * (kStep / 8) * kUnit);
                 now = next;
             }
             // one barrier a tile: who writes a part again has passed the next tile's, and so have all who read it
@@ -370,7 +380,7 @@ w4_matvec_kernel(MatvecArgs p)
                 ask(step + 1);
                 fetch(blockIdx.x, step + 1, next);
             }
-            multiply(now, lds + (step & 1) * kBuffer);
+            multiply(now, step, lds + (step & 1) * kBuffer);
             if (more) put(step + 1);                     // last read two steps ago, before the barrier that ended that step
             now = next;
             __syncthreads();
