@@ -8,13 +8,14 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgqsgd.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("common.hip", "norm.hip", "quantize.hip", "aggregate.hip", "reduce.hip",
-                                           "sparse.hip", "pipeline.hip", "dropout.hip", "rms_norm.hip", "weights.hip", "matvec.hip")]
+                                           "sparse.hip", "pipeline.hip", "dropout.hip", "rms_norm.hip", "weights.hip", "matvec.hip",
+                                           "matvec_bf16.hip", "matvec_f16.hip", "matvec_i8.hip")]
 MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 # for a test: gq_compact with a third of its spans mute (GQ_MUTE_SPANS in sparse.hip); nothing else loads it
 MUTE_LIB = os.path.join(HERE, "libgqsgd_mute.so")
 MUTE_SOURCES = [os.path.join(CSRC, f) for f in ("common.hip", "sparse.hip")]
-HEADERS = [os.path.join(CSRC, "gq_device.hpp"), os.path.join(CSRC, "gq_host.hpp"), os.path.join(CSRC, "gq_layers.hpp"),
+HEADERS = [os.path.join(CSRC, "gq_device.hpp"), os.path.join(CSRC, "gq_host.hpp"), os.path.join(CSRC, "gq_layers.hpp"), os.path.join(CSRC, "matvec.hpp"),
            os.path.join(ROOT, "include", "gqsgd.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,432 +1,16 @@
-// Rows of activations times 4-bit weights under group scales, on the matrix cores.
+// Rows of activations times 4-bit weights under group scales.
 // The contract of the entry point is stated in include/gqsgd.h.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stddef.h>
 
 #include "gqsgd.h"
-#include "gq_layers.hpp"
+#include "matvec.hpp"
 
-namespace gq {
-
-// What an activation type brings along.  A lane's eight codes are one word; the instructions take them as eight activations'
-// worth of operand B, and x as operand A in the order in which unfolding leaves the codes:
-//   16 bits  pairs (i, i + 4): one shift and one v_and_or_b32 put nibbles i and i + 4 of (word ^ 0x88..8) behind the exponent of
-//            16.0 of two halves, which are then 16 + (code + 8) = 24 + code exactly.  24 times the sum of x is taken out again by
-//            the same instruction with a constant operand of -24.
-//   int8     bytes of 16 times a code, even ones (word << 4) and odd ones (word) under 0xF0F0F0F0: three instructions for eight
-//            codes; sums are exact integers.
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-template <typename X> struct Act;
-template <typename V, uint32_t ONE, int TOP, uint32_t MINUS> struct Act16 {
-    typedef V Operand;
-    typedef f32x4 Sum;
-    static constexpr bool kMoved = true;
-    static constexpr float kUnit = 1.0f;
-    static __device__ __forceinline__ Operand unfold(uint32_t w)
-    {
-        const uint32_t u = w ^ 0x88888888u, mask = 0x000F000Fu << TOP;
-        const u32x4 r = {((u << TOP) & mask) | ONE, ((TOP >= 4 ? u << (TOP - 4) : u >> (4 - TOP)) & mask) | ONE,
-                         ((TOP >= 8 ? u << (TOP - 8) : u >> (8 - TOP)) & mask) | ONE, ((u >> (12 - TOP)) & mask) | ONE};
-        return __builtin_bit_cast(Operand, r);
-    }
-    static __device__ __forceinline__ Operand minus24() { return __builtin_bit_cast(Operand, u32x4{MINUS, MINUS, MINUS, MINUS}); }
-    // eight activations as they lie in memory, and in the order of unfold()
-    typedef u32x4 Raw;
-    typedef uint16_t Bits;
-    static __device__ __forceinline__ Raw ordered(Raw v)
-    {
-        return Raw{(v.x & 0xFFFFu) | (v.z << 16), (v.x >> 16) | (v.z & 0xFFFF0000u), (v.y & 0xFFFFu) | (v.w << 16), (v.y >> 16) | (v.w & 0xFFFF0000u)};
-    }
-};
-template <> struct Act<bf16> : Act16<bf16x8, 0x41804180u, 3, 0xC1C0C1C0u> {
-    static __device__ __forceinline__ Sum product(Operand a, Operand b, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-};
-template <> struct Act<f16> : Act16<f16x8, 0x4C004C00u, 6, 0xCE00CE00u> {
-    static __device__ __forceinline__ Sum product(Operand a, Operand b, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-};
-template <> struct Act<int8_t> {
-    typedef long Operand;
-    typedef i32x4 Sum;
-    static constexpr bool kMoved = false;
-    static constexpr float kUnit = 0.0625f;
-    static __device__ __forceinline__ Operand unfold(uint32_t w)
-    {
-        return __builtin_bit_cast(Operand, u32x2{(w << 4) & 0xF0F0F0F0u, w & 0xF0F0F0F0u});
-    }
-    static __device__ __forceinline__ Sum product(Operand a, Operand b, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ Operand minus24() { return 0; }
-    typedef u32x2 Raw;
-    typedef uint8_t Bits;
-    static __device__ __forceinline__ Raw ordered(Raw v)
-    {
-        return Raw{__builtin_amdgcn_perm(v.y, v.x, 0x06040200u), __builtin_amdgcn_perm(v.y, v.x, 0x07050301u)};
-    }
-};
-
-// d[j] of lane group q (lanes 16 q .. 16 q + 15) becomes d[q] of lane group j
-__device__ __forceinline__ void transpose4(uint32_t *d)
-{
-    const auto a = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
-    const auto b = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
-    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-    const auto e = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    d[0] = c[0]; d[1] = c[1]; d[2] = e[0]; d[3] = e[1];
-}
-
-struct MatvecArgs {
-    const void *x;
-    const float *x_scales;
-    const uint8_t *codes;
-    const void *scales, *bias;
-    void *y;
-    int64_t row_bytes;
-    int m, rows, cols, groups, y_dtype;
-    int row_shift;        // a row of staged x in LDS has 2^row_shift columns
-};
-
-// A workgroup of WN x WK waves owns WN * RT * 16 rows of the weights at a time and up to MT * 16 rows of x; the WK waves share out
-// the columns, 128 U at a time (a step), and their sums are joined in LDS at a tile's end.  x is staged in LDS: RESIDENT, all of
-// it, once, for all tiles of rows that the workgroup takes in turn; otherwise a step's columns at a time into two buffers in
-// turn, the next step's loads in flight meanwhile, and the workgroup takes one tile.
-template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WN * WK)
-w4_matvec_kernel(MatvecArgs p)
-{
-    typedef Act<X> A;
-    typedef typename A::Operand Operand;
-    typedef typename A::Sum Sum;
-    typedef typename A::Raw Raw;
-    typedef typename A::Bits Bits;
-    constexpr int kThreads = 64 * WN * WK, kUnit = 8 * (int)sizeof(X), kSwizzle = 128 / kUnit - 1;
-    constexpr int kGroups = 128 / GROUP, kBlocks = GROUP / 32, kStep = 128 * U * WK;
-    constexpr int kPerWave = MT * RT * 256, kPart = WN * WK * kPerWave;            // floats of the waves' sums
-    constexpr int kBuffer = MT * 16 * kStep * (int)sizeof(X);
-    constexpr int kAhead = MT * 16 * (kStep / 8) / kThreads;                       // units of a step's x per lane
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wk = wave % WK, wn = wave / WK;
-    const int i16 = lane & 15, q = lane >> 4;
-    const int first_m = blockIdx.y * MT * 16, m_rows = min(p.m - first_m, MT * 16);
-    const X *x = (const X *)p.x + (int64_t)first_m * p.cols;
-    const int tiles = (p.rows + WN * RT * 16 - 1) / (WN * RT * 16), steps = (p.cols + kStep - 1) / kStep;
-
-    // ---- x: units of eight columns, in the order in which the codes unfold ----
-    auto load_unit = [&](int row, int c) {
-        Raw v;
-        const X *at = x + (int64_t)row * p.cols + c;
-        if (c + 8 <= p.cols) {
-            __builtin_memcpy(&v, at, sizeof(v));
-        } else {
-            constexpr int kBits = 8 * (int)sizeof(X), kWord = 32 / kBits;
-            v = Raw{};
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (c + i < p.cols) v[i / kWord] |= (uint32_t) reinterpret_cast<const Bits *>(at)[i] << (kBits * (i % kWord));
-        }
-        return v;
-    };
-    // v without its first `over` elements, zeros behind; v itself for over <= 0
-    auto drop_low = [&](Raw v, int over) {
-        if (over <= 0) return v;
-        constexpr int kWords = sizeof(Raw) / 4, kBits = 8 * (int)sizeof(X);
-        const int bits = min(over, 8) * kBits, words = bits / 32, rest = bits % 32;
-        uint32_t w[2 * kWords + 1];
-#pragma unroll
-        for (int i = 0; i <= 2 * kWords; i++) w[i] = i < kWords ? v[i] : 0u;
-        Raw o;
-#pragma unroll
-        for (int i = 0; i < kWords; i++) {
-            uint32_t lo = 0, hi = 0;
-#pragma unroll
-            for (int k = 0; k <= kWords; k++) {
-                lo = words == k ? w[i + k] : lo;
-                hi = words == k ? w[i + k + 1] : hi;
-            }
-            o[i] = (uint32_t)((((uint64_t)hi << 32) | lo) >> rest);
-        }
-        return o;
-    };
-    auto store_unit = [&](uint8_t *to, int row, int unit, int shift, Raw v) {
-        *reinterpret_cast<Raw *>(to + ((row << shift) + (unit ^ (row & kSwizzle))) * kUnit) = A::ordered(v);
-    };
-    const int shift = RESIDENT ? p.row_shift - 3 : __builtin_ctz(kStep / 8);       // of units a row
-    // where a lane finds operand A: unit 16 chunk + (4 j + q), or (4 q + j) for groups of 128, of its row; a chunk is 128 columns.
-    // Rows of x that are not there are the last one again and end in rows of y that are not there.
-    int from[4];
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const int r = RESIDENT ? min(i16, m_rows - 1) : i16;
-        from[j] = ((r << shift) + ((GROUP < 128 ? 4 * j + q : 4 * q + j) ^ (r & kSwizzle))) * kUnit;
-    }
-    constexpr int kTileBytes = 16 * kStep * (int)sizeof(X);                        // of 16 rows of x, streamed
-
-    // ---- codes and scales of a step: 16 bytes of codes a lane and chunk, the scales of its row's chunks in one load ----
-    // Both stay as they lie in memory until they are used: a conversion here would be waited for here.
-    constexpr int kScales = U * kGroups, kScaleWords = (kScales * (int)sizeof(S) + 3) / 4;
-    struct Fetched { u32x4 w[U][RT]; uint32_t s[RT][kScaleWords]; };
-    const uint32_t scale_bytes = (uint32_t)(p.groups * (int)sizeof(S));
-    const int last_block = (p.cols - 1) / 32;
-    // the first scale of a step's load: where the step runs over the row's end, so early that the load does not
-    auto first_scale = [&](int step) { return min((step * WK + wk) * kScales, max(p.groups - kScales, 0)); };
-    auto fetch = [&](int tile, int step, Fetched &f) {
-        // The wave's first row is the same for all lanes, what differs is a lane's row within the tile.  A wave whose rows all lie past
-        // the last one reads that one, and so do rows past it: never stored.
-        const int first = min((tile * WN + wn) * RT * 16, p.rows - 1), c = (step * WK + wk) * U * 128;
-        const uint8_t *codes = p.codes + (int64_t)first * p.row_bytes;
-        const uint8_t *scales = (const uint8_t *)p.scales + ((int64_t)first * p.groups + first_scale(step)) * (int)sizeof(S);
-        const int last = p.rows - 1 - first;
-#pragma unroll
-        for (int t = 0; t < RT; t++) {
-            const uint32_t r = (uint32_t)min(16 * t + i16, last), at = r * (uint32_t)p.row_bytes;
-            // past the row's end the last codes again, where x is zero
-#pragma unroll
-            for (int u = 0; u < U; u++)
-                f.w[u][t] = *reinterpret_cast<const u32x4 *>(codes + (at + 16u * (uint32_t)min(c / 32 + 4 * u + q, last_block)));
-            if (p.groups >= kScales) {
-                if constexpr (kScaleWords * 4 != kScales * (int)sizeof(S)) f.s[t][kScaleWords - 1] = 0;
-                __builtin_memcpy(f.s[t], scales + r * scale_bytes, kScales * sizeof(S));
-            } else {                                                               // few columns
-                typedef typename std::conditional<sizeof(S) == 4, uint32_t, uint16_t>::type Bits;
-                constexpr int kPer = 4 / (int)sizeof(S);
-                const Bits *from_row = reinterpret_cast<const Bits *>(scales + r * scale_bytes);
-#pragma unroll
-                for (int j = 0; j < kScaleWords; j++) {
-                    f.s[t][j] = 0;
-#pragma unroll
-                    for (int i = 0; i < kPer; i++)
-                        if (j * kPer + i < p.groups) f.s[t][j] |= (uint32_t)from_row[j * kPer + i] << (16 * i);
-                }
-            }
-        }
-    };
-    // a step's scales as numbers, zeros behind the row's end
-    auto scales_of = [&](const uint32_t *words, int step, float *s) {
-#pragma unroll
-        for (int k = 0; k < kScales; k++) {
-            if constexpr (sizeof(S) == 4) s[k] = __uint_as_float(words[k]);
-            else s[k] = __uint_as_float((k & 1) ? words[k / 2] & 0xFFFF0000u : words[k / 2] << 16);
-        }
-        // what the load began too early, or what lies behind the row's end where it could not begin earlier
-        for (int late = min((step * WK + wk) * kScales - first_scale(step), kScales); late > 0; late--) {
-#pragma unroll
-            for (int k = 0; k < kScales; k++) s[k] = k + 1 < kScales ? s[k + 1] : 0.0f;
-        }
-    };
-
-    f32x4 acc[MT][RT];
-    auto clear = [&] {
-#pragma unroll
-        for (int i = 0; i < MT; i++)
-#pragma unroll
-            for (int t = 0; t < RT; t++) acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    };
-    // a step's products; `staged`: where its first column is
-    auto multiply = [&](const Fetched &f, int step, const uint8_t *staged) {
-        float scale[RT][kScales];
-#pragma unroll
-        for (int t = 0; t < RT; t++) scales_of(f.s[t], step, scale[t]);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const uint8_t *chunk = staged + (wk * U + u) * 16 * kUnit;
-            uint32_t d[RT][4];
-#pragma unroll
-            for (int t = 0; t < RT; t++) {
-#pragma unroll
-                for (int j = 0; j < 4; j++) d[t][j] = f.w[u][t][j];
-                // operand j of the whole wave has to lie within a group: a group of 128 takes word j of each lane as it comes
-                if (GROUP < 128) transpose4(d[t]);
-            }
-#pragma unroll
-            for (int g = 0; g < kGroups; g++) {
-                Operand a[MT][kBlocks];
-                Sum start[MT];
-#pragma unroll
-                for (int i = 0; i < MT; i++) {
-                    start[i] = Sum{};
-#pragma unroll
-                    for (int j = 0; j < kBlocks; j++) {
-                        a[i][j] = *reinterpret_cast<const Operand *>(chunk + from[g * kBlocks + j] + i * kTileBytes);
-                        if (A::kMoved) start[i] = A::product(a[i][j], A::minus24(), start[i]);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < RT; t++) {
-                    Operand b[kBlocks];
-#pragma unroll
-                    for (int j = 0; j < kBlocks; j++) b[j] = A::unfold(d[t][g * kBlocks + j]);
-#pragma unroll
-                    for (int i = 0; i < MT; i++) {
-                        Sum s = start[i];
-#pragma unroll
-                        for (int j = 0; j < kBlocks; j++) s = A::product(a[i][j], b[j], s);
-#pragma unroll
-                        for (int r = 0; r < 4; r++) acc[i][t][r] = __builtin_fmaf((float)s[r], scale[t][u * kGroups + g], acc[i][t][r]);
-                    }
-                }
-                // the groups one after another, sums and all: left to itself the compiler moves all sums behind all products, and
-                // the products of all groups at once are more than the registers that there are
-                if (MT * RT > 1) {
-#pragma unroll
-                    for (int i = 0; i < MT; i++)
-#pragma unroll
-                        for (int t = 0; t < RT; t++) asm volatile("" : "+v"(acc[i][t]));
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        }
-    };
-    // the waves that shared out the columns leave their sums in `part`; element (m 4 q + r, row i16) of a tile is lane 16 q + i16's r-th
-    auto leave = [&](float *part) {
-#pragma unroll
-        for (int i = 0; i < MT; i++)
-#pragma unroll
-            for (int t = 0; t < RT; t++)
-                *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + ((i * RT + t) * 64 + lane) * 4) = acc[i][t];
-    };
-    auto join = [&](const float *part, int tile_of_rows) {
-        for (int e = threadIdx.x; e < WN * kPerWave; e += kThreads) {
-            // e: (wave of rows, tile, m within it, row within it), the row fastest
-            const int w = e / kPerWave, tile = e % kPerWave / 256, mi = e % 256 / 16, ri = e % 16;
-            const int mm = first_m + tile / RT * 16 + mi, row = (tile_of_rows * WN + w) * RT * 16 + tile % RT * 16 + ri;
-            if (mm >= p.m || row >= p.rows) continue;
-            float v = 0.0f;
-#pragma unroll
-            for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
-            if (p.x_scales) v *= A::kUnit * p.x_scales[mm];
-            const int64_t at = (int64_t)mm * p.rows + row;
-            if (p.y_dtype == GQ_F32) ((float *)p.y)[at] = p.bias ? v + ((const float *)p.bias)[row] : v;
-            else if (p.y_dtype == GQ_BF16) ((bf16 *)p.y)[at] = (bf16)(p.bias ? v + (float)((const bf16 *)p.bias)[row] : v);
-            else ((f16 *)p.y)[at] = (f16)(p.bias ? v + (float)((const f16 *)p.bias)[row] : v);
-        }
-    };
-
-    Fetched now, next;
-    if constexpr (RESIDENT) {
-        // the first units of x are asked for before the codes: loads come back in order, and x is wanted first
-        const int units = m_rows << shift;
-        constexpr int kFirst = 2;
-        Raw v[kFirst];
-#pragma unroll
-        for (int i = 0; i < kFirst; i++) {
-            const int u = min((int)threadIdx.x + i * kThreads, units - 1);
-            v[i] = load_unit(u >> shift, (u & ((1 << shift) - 1)) * 8);
-        }
-        if (steps > 0) fetch(blockIdx.x, 0, now);
-#pragma unroll
-        for (int i = 0; i < kFirst; i++) {
-            const int u = (int)threadIdx.x + i * kThreads;
-            if (u < units) store_unit(lds, u >> shift, u & ((1 << shift) - 1), shift, v[i]);
-        }
-        for (int u = threadIdx.x + kFirst * kThreads; u < units; u += kThreads)
-            store_unit(lds, u >> shift, u & ((1 << shift) - 1), shift, load_unit(u >> shift, (u & ((1 << shift) - 1)) * 8));
-        __syncthreads();
-        float *parts = reinterpret_cast<float *>(lds + units * kUnit);             // two, in turn
-        int turn = 0;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
-            clear();
-            for (int step = 0; step < steps; step++) {
-                const bool more = step + 1 < steps;
-                if (more || tile + (int)gridDim.x < tiles) fetch(more ? tile : tile + gridDim.x, more ? step + 1 : 0, next);
-                multiply(now, step, lds + step * (kStep / 8) * kUnit);
-                now = next;
-            }
-            // one barrier a tile: who writes a part again has passed the next tile's, and so have all who read it
-            leave(parts + turn * kPart);
-            __syncthreads();
-            join(parts + turn * kPart, tile);
-        }
-    } else {
-        // a lane's units are in one column of units, kRowsApart rows apart; rows that are not there hold the last one again
-        constexpr int kRowUnits = kStep / 8, kRowsApart = kThreads / kRowUnits;
-        static_assert(kThreads % kRowUnits == 0 && kAhead * kRowsApart == MT * 16, "units of a step");
-        const int unit = threadIdx.x % kRowUnits, row0 = threadIdx.x / kRowUnits;
-        Raw ahead[kAhead];
-        // a unit that runs over the row's end (or lies past it) is read so that it ends there, and moved into place in put()
-        auto ask = [&](int step) {
-            const int c = min(step * kStep + 8 * unit, p.cols - 8);
-            if (p.cols >= 8) {
-#pragma unroll
-                for (int i = 0; i < kAhead; i++)
-                    __builtin_memcpy(&ahead[i], x + (uint32_t)(min(row0 + i * kRowsApart, m_rows - 1) * p.cols + c), sizeof(Raw));
-            }
-        };
-        auto put = [&](int step) {
-            uint8_t *to = lds + (step & 1) * kBuffer;
-            if (p.cols < 8) {
-                for (int i = 0; i < kAhead; i++)
-                    store_unit(to, row0 + i * kRowsApart, unit, shift, load_unit(min(row0 + i * kRowsApart, m_rows - 1), 8 * unit));
-                return;
-            }
-            if ((step + 1) * kStep > p.cols) {
-                const int over = step * kStep + 8 * unit - (p.cols - 8);           // elements to drop from the low end
-#pragma unroll
-                for (int i = 0; i < kAhead; i++) ahead[i] = drop_low(ahead[i], over);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; i++) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
-        };
-        clear();
-        if (steps > 0) {
-            ask(0);
-            fetch(blockIdx.x, 0, now);
-            put(0);
-        }
-        __syncthreads();
-        for (int step = 0; step < steps; step++) {
-            const bool more = step + 1 < steps;
-            if (more) {
-                ask(step + 1);
-                fetch(blockIdx.x, step + 1, next);
-            }
-            multiply(now, step, lds + (step & 1) * kBuffer);
-            if (more) put(step + 1);                     // last read two steps ago, before the barrier that ended that step
-            now = next;
-            __syncthreads();
-        }
-        float *part = reinterpret_cast<float *>(lds);
-        leave(part);
-        __syncthreads();
-        join(part, blockIdx.x);
-    }
-}
-
-constexpr int kLds = 64 * 1024;
-constexpr int kResidentGrid = 768;
-
-template <typename X, typename S, int GROUP, int MT, int RT, int WN, int WK, int U, bool RESIDENT>
-static gq_status launch_matvec(MatvecArgs p, hipStream_t stream)
-{
-    constexpr int kStep = 128 * U * WK, kParts = WN * WK * MT * RT * 1024, kRows = WN * RT * 16;
-    int64_t bx = ((int64_t)p.rows + kRows - 1) / kRows;
-    const int64_t by = ((int64_t)p.m + MT * 16 - 1) / (MT * 16);
-    unsigned lds;
-    if (RESIDENT) {
-        lds = (unsigned)((p.m << p.row_shift) * (int)sizeof(X) + 2 * kParts);
-        if (bx > kResidentGrid) bx = kResidentGrid;
-    } else {
-        lds = 2 * MT * 16 * kStep * (int)sizeof(X);
-        if (lds < kParts) lds = kParts;
-    }
-    if (!grid_fits(bx, 64 * WN * WK) || by > 65535) return GQ_ERR_INVALID_ARG;
-    w4_matvec_kernel<X, S, GROUP, MT, RT, WN, WK, U, RESIDENT><<<dim3((unsigned)bx, (unsigned)by), 64 * WN * WK, lds, stream>>>(p);
-    return launched();
-}
-
-template <typename X, typename S, int GROUP> static gq_status matvec_by_rows(MatvecArgs p, hipStream_t stream)
-{
-    if (p.m <= 16) {
-        p.row_shift = 11;                                                          // whole steps of 2048 columns
-        while ((1 << p.row_shift) < p.cols) p.row_shift++;
-        if (((int64_t)p.m << p.row_shift) * (int)sizeof(X) <= kLds - 16 * 1024) return launch_matvec<X, S, GROUP, 1, 1, 1, 8, 2, true>(p, stream);
-    }
-    if (p.m <= 16 || p.rows <= 2048) return launch_matvec<X, S, GROUP, 1, 1, 4, 2, 4, false>(p, stream);
-    if (p.m <= 32) return launch_matvec<X, S, GROUP, 2, 2, 2, 4, 1, false>(p, stream);
-    return launch_matvec<X, S, GROUP, 4, 2, 2, 4, 1, false>(p, stream);
-}
-
-}  // namespace gq
+// compiled in files of their own
+extern template gq_status gq::matvec<gq::bf16>(const gq::MatvecArgs &, int, int, hipStream_t);
+extern template gq_status gq::matvec<gq::f16>(const gq::MatvecArgs &, int, int, hipStream_t);
+extern template gq_status gq::matvec<int8_t>(const gq::MatvecArgs &, int, int, hipStream_t);
 
 using namespace gq;
 
@@ -444,12 +28,6 @@ extern "C" gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t 
     const MatvecArgs p = {x, x_scales, (const uint8_t *)codes, scales, bias, y, gq_w4_row_bytes(cols), (int)m, (int)rows, (int)cols,
                           (int)((cols + group - 1) / group), (int)y_dtype, 0};
     const hipStream_t stream = (hipStream_t)hip_stream;
-    return with_scale_type(scale_dtype, [&](auto s) {
-        typedef decltype(s) S;
-        auto go = [&](auto t) {
-            typedef decltype(t) X;
-            return group == 32 ? matvec_by_rows<X, S, 32>(p, stream) : group == 64 ? matvec_by_rows<X, S, 64>(p, stream) : matvec_by_rows<X, S, 128>(p, stream);
-        };
-        return x_dtype == GQ_BF16 ? go(bf16()) : x_dtype == GQ_F16 ? go(f16()) : go(int8_t());
-    });
+    return x_dtype == GQ_BF16 ? matvec<bf16>(p, group, scale_dtype, stream)
+           : x_dtype == GQ_F16 ? matvec<f16>(p, group, scale_dtype, stream) : matvec<int8_t>(p, group, scale_dtype, stream);
 }

@@ -1,0 +1,9 @@
+// gq_w4_matvec for activations in bfloat16.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+
+#include "gqsgd.h"
+#include "matvec.hpp"
+
+template gq_status gq::matvec<gq::bf16>(const gq::MatvecArgs &, int, int, hipStream_t);
