@@ -15,7 +15,7 @@ constexpr int64_t kLongDropout = 1 << 21;
 
 // A lane owns UNITS units, each of eight columns of one row and one (16 bits) or two (32 bits) Philox calls.  All loads are asked
 // for before the first draw.
-template <typename T, bool SHORT, bool RESIDUAL, bool TINY, int UNITS>
+template <typename T, bool SHORT, bool RESIDUAL, bool TINY, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 dropout_kernel(const T *x, const T *residual, T *out, int64_t rows, uint32_t per_row, int64_t n, Drop drop)
 {
@@ -23,8 +23,8 @@ dropout_kernel(const T *x, const T *residual, T *out, int64_t rows, uint32_t per
     Eight<T> v[UNITS], r[UNITS];
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
-        at[k] = row_unit<UNITS>(blockIdx.x, k, per_row);
-        const int64_t c = (int64_t)at[k].unit * 8, row = at[k].row < rows ? at[k].row : rows - 1;
+        at[k] = row_unit<UNITS, FLAT>(blockIdx.x, k, per_row);
+        const int64_t c = (int64_t)at[k].unit * 8, row = FLAT ? 0 : at[k].row < rows ? at[k].row : rows - 1;
         ask8<true, TINY>(x + row * n, n, c, v[k]);
         if (RESIDUAL) ask8<true, TINY>(residual + row * n, n, c, r[k]);
     }
@@ -37,12 +37,13 @@ dropout_kernel(const T *x, const T *residual, T *out, int64_t rows, uint32_t per
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) f[i] = v[k].f(i);
-        drop8<SHORT>(drop, drop.first + ((uint64_t)at[k].row * per_row + at[k].unit) * 8, f);
+        const int64_t row = FLAT ? 0 : at[k].row;
+        drop8<SHORT>(drop, drop.first + ((uint64_t)row * per_row + at[k].unit) * 8, f);
         if (RESIDUAL) {
 #pragma unroll
             for (int i = 0; i < 8; i++) f[i] = r[k].f(i) + f[i];
         }
-        store8(out + at[k].row * n + c, n - c, f);
+        store8(out + row * n + c, n - c, f);
     }
 }
 
@@ -58,6 +59,8 @@ extern "C" gq_status gq_dropout(const void *x, const void *residual, int64_t row
     if (st != GQ_OK) return st;
     if (rows == 0 || n == 0) return GQ_OK;
     if (!aligned(x, 16) || !aligned(out, 16) || !aligned_or_null(residual, 16)) return GQ_ERR_INVALID_ARG;
+    const bool flat = n >= 8 && (rows == 1 || n % 8 == 0) && flat_fits(rows * (pitch8(n) / 8));      // whole units a row
+    if (flat) n *= rows, rows = 1;
     const int64_t per_row = pitch8(n) / 8, units = rows * per_row;
     const bool four = n >= 8 && units >= kLongDropout;
     const int64_t per_block = (four ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
@@ -67,8 +70,9 @@ extern "C" gq_status gq_dropout(const void *x, const void *residual, int64_t row
         typedef decltype(t) T;
         auto go = [&](auto shorter, auto with_residual) {
             constexpr bool SHORT = decltype(shorter)::value, RESIDUAL = decltype(with_residual)::value;
-            auto kernel = n < 8 ? dropout_kernel<T, SHORT, RESIDUAL, true, 1>
-                          : four ? dropout_kernel<T, SHORT, RESIDUAL, false, 4> : dropout_kernel<T, SHORT, RESIDUAL, false, 1>;
+            auto kernel = n < 8 ? dropout_kernel<T, SHORT, RESIDUAL, true, false, 1>
+                          : flat ? (four ? dropout_kernel<T, SHORT, RESIDUAL, false, true, 4> : dropout_kernel<T, SHORT, RESIDUAL, false, true, 1>)
+                                 : (four ? dropout_kernel<T, SHORT, RESIDUAL, false, false, 4> : dropout_kernel<T, SHORT, RESIDUAL, false, false, 1>);
             kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)x, (const T *)residual, (T *)out, rows, (uint32_t)per_row, n, d);
             return launched();
         };

@@ -113,15 +113,21 @@ template <typename T> __device__ __forceinline__ void store8(T *p, int64_t left,
 }
 
 // Row and unit within it of a lane's k-th unit, where rows have `per_row` units and a workgroup takes UNITS * kBlock of them: one
-// 64-bit division a workgroup, on the scalar unit, and a 32-bit one a unit.  The row may lie past the last one.
+// 64-bit division a workgroup, on the scalar unit, and a 32-bit one a unit.  FLAT: all is one row of less than 2^31 units (whole units a
+// row make a matrix one), nothing is divided.  The row may lie past the last one.
 struct RowUnit { int64_t row; uint32_t unit; };
-template <int UNITS> __device__ __forceinline__ RowUnit row_unit(uint32_t block, int k, uint32_t per_row)
+template <int UNITS, bool FLAT> __device__ __forceinline__ RowUnit row_unit(uint32_t block, int k, uint32_t per_row)
 {
+    if constexpr (FLAT) {
+        const uint32_t u = block * (UNITS * kBlock) + (uint32_t)k * kBlock + threadIdx.x;
+        return {u >= per_row, u};
+    }
     const uint64_t first = (uint64_t)block * (UNITS * kBlock), row = first / per_row;
     const uint32_t at = (uint32_t)(first - row * per_row) + (uint32_t)k * kBlock + threadIdx.x;    // below 2^28 + 2^12 for a matrix that fits
     const uint32_t more = at / per_row;
     return {(int64_t)row + more, at - more * per_row};
 }
+static inline bool flat_fits(int64_t units) { return units < 0x7FFFFFFF - 4096; }
 
 // The dropout decision of gq_dropout_params, as the kernels take it.
 struct Drop {

@@ -9,33 +9,49 @@
 
 namespace gq {
 
-// w / scale to the nearest integer, ties to even, of the exact quotient: the product with fl32(1 / scale) is off by less than
-// 2^-22 and so rounds to the nearest integer or, next to a border, its neighbour.  w - q scale is exact there (it is a multiple of
-// half an ulp of scale and below scale), and says which.
+// w / scale to the nearest integer, ties to even, of the exact quotient: the product with 1 / scale (to 2^-22) rounds to the nearest
+// integer q or, next to a border, its neighbour.  w - q scale is exact there (it is a multiple of half an ulp of scale and below scale),
+// and says which.  The largest magnitude of the group is 7 scale to within scale's rounding, so 7 is not passed.
 __device__ __forceinline__ float code_of_quotient(float w, float scale, float inv)
 {
-    float q = __builtin_rintf(w * inv);
-    const float r = __builtin_fmaf(-q, scale, w), twice = 2.0f * __builtin_fabsf(r);
-    const bool odd = (int)q & 1;
-    if (twice > scale || (twice == scale && odd)) q += __builtin_copysignf(1.0f, r);
-    return __builtin_amdgcn_fmed3f(q, -7.0f, 7.0f);
+    const float q = __builtin_rintf(w * inv), r = __builtin_fmaf(-q, scale, w);
+    const float over = __builtin_fmaf(__builtin_fabsf(r), 2.0f, -scale);      // beyond the border, on it, or short of it
+    // q + 0.75 goes to the next integer, q + 0.5 to the even one
+    const float by = over > 0.0f ? 0.75f : over == 0.0f ? 0.5f : 0.0f;
+    return __builtin_rintf(q + __builtin_copysignf(by, r));
 }
 
 template <typename S> struct GroupScale { S stored; float scale, inv; };
 template <typename S> __device__ __forceinline__ GroupScale<S> group_scale(uint32_t top_bits)
 {
     if (top_bits >= 0x7F800000u) return {(S)__builtin_nanf(""), 0.0f, 0.0f};
-    const S stored = (S)(__uint_as_float(top_bits) / 7.0f);
-    const float scale = (float)stored, inv = 1.0f / scale;
-    if (!(inv <= 3.402823466e+38f)) return {(S)0.0f, 0.0f, 0.0f};
-    return {stored, scale, inv};
+    // a / 7: a times the rounded 1/7 and one correction is the correctly rounded quotient (verified over all 2^23 mantissas), far
+    // enough from the smallest numbers; there, the division itself
+    const float a = __uint_as_float(top_bits), sevenths = 1.0f / 7.0f;
+    const float q0 = a * sevenths;
+    const float seventh = a >= 0x1p-90f ? __builtin_fmaf(__builtin_fmaf(-7.0f, q0, a), sevenths, q0) : a / 7.0f;
+    const S stored = (S)seventh;
+    const float scale = (float)stored;
+    if (!(scale > 0x1p-128f)) return {(S)0.0f, 0.0f, 0.0f};                   // 1 / scale is not finite
+    return {stored, scale, scale >= 0x1p-120f ? __builtin_amdgcn_rcpf(scale) : 1.0f / scale};   // an ulp does not matter to the codes
+}
+
+// Eight codes -7 .. 7 as nibbles, four at a time put together as floats (exact below 2^24) and converted together: a bias of 8 in
+// every field keeps the sum non-negative, flipping the fields' top bits takes it out again.
+__device__ __forceinline__ uint32_t eight_nibbles(const float *q)
+{
+    uint32_t half[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+        half[h] = (uint32_t)__builtin_fmaf(q[4 * h + 3], 4096.0f, __builtin_fmaf(q[4 * h + 2], 256.0f, __builtin_fmaf(q[4 * h + 1], 16.0f, q[4 * h] + 34952.0f)));
+    return (half[0] | (half[1] << 16)) ^ 0x88888888u;
 }
 
 // A lane owns UNITS units, each of eight consecutive columns (16 or 32 bytes of weights, one word of codes), a group is 4, 8 or 16
 // neighbouring lanes: the maximum goes round them by DPP within a row of 16 lanes.  Units past the row's last column (a row
 // is padded to whole groups of units) hold zeros; those within the padding of the row's codes write them.  Bound by memory: read
 // once, written once.
-template <typename T, typename S, int GROUP, bool TINY, int UNITS>
+template <typename T, typename S, int GROUP, bool TINY, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per_row, int groups, uint32_t row_words, uint32_t *codes, S *scales)
 {
@@ -43,8 +59,8 @@ group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per
     Eight<T> x[UNITS];
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
-        at[k] = row_unit<UNITS>(blockIdx.x, k, units_per_row);
-        ask8<true, TINY>(w + (at[k].row < rows ? at[k].row : rows - 1) * cols, cols, (int64_t)at[k].unit * 8, x[k]);
+        at[k] = row_unit<UNITS, FLAT>(blockIdx.x, k, units_per_row);
+        ask8<true, TINY>(FLAT ? w : w + (at[k].row < rows ? at[k].row : rows - 1) * cols, cols, (int64_t)at[k].unit * 8, x[k]);
     }
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
@@ -63,18 +79,21 @@ group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per
         const GroupScale<S> gs = group_scale<S>(m);
         uint32_t word = 0;
         if (gs.inv != 0.0f) {
+            float q[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) word |= ((uint32_t)(int)code_of_quotient(v[i], gs.scale, gs.inv) & 15u) << (4 * i);
+            for (int i = 0; i < 8; i++) q[i] = code_of_quotient(v[i], gs.scale, gs.inv);
+            word = eight_nibbles(q);
         }
         if (at[k].row < rows) {
-            if (at[k].unit < row_words) __builtin_nontemporal_store(word, codes + at[k].row * row_words + at[k].unit);
-            if (at[k].unit % (GROUP / 8) == 0) scales[at[k].row * groups + at[k].unit / (GROUP / 8)] = gs.stored;
+            const int64_t row = FLAT ? 0 : at[k].row;
+            if (FLAT || at[k].unit < row_words) __builtin_nontemporal_store(word, codes + row * row_words + at[k].unit);
+            if (at[k].unit % (GROUP / 8) == 0) scales[row * groups + at[k].unit / (GROUP / 8)] = gs.stored;
         }
     }
 }
 
 // The same units.
-template <typename T, typename S, int UNITS>
+template <typename T, typename S, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, uint32_t units_per_row, int group_shift, int groups,
                         uint32_t row_words, T *out)
@@ -84,10 +103,11 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
     S scale[UNITS];
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
-        at[k] = row_unit<UNITS>(blockIdx.x, k, units_per_row);
-        const int64_t row = at[k].row < rows ? at[k].row : rows - 1;
-        word[k] = __builtin_nontemporal_load(codes + row * row_words + at[k].unit);
-        scale[k] = scales[row * groups + (at[k].unit >> (group_shift - 3))];
+        at[k] = row_unit<UNITS, FLAT>(blockIdx.x, k, units_per_row);
+        const int64_t row = FLAT ? 0 : at[k].row < rows ? at[k].row : rows - 1;
+        const uint32_t unit = FLAT ? min(at[k].unit, units_per_row - 1) : at[k].unit;
+        word[k] = __builtin_nontemporal_load(codes + row * row_words + unit);
+        scale[k] = scales[row * groups + (unit >> (group_shift - 3))];
     }
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
@@ -95,7 +115,7 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = (float)((int)(word[k] << (28 - 4 * i)) >> 28) * (float)scale[k];
-        store8(out + at[k].row * cols + (int64_t)at[k].unit * 8, cols - (int64_t)at[k].unit * 8, v);
+        store8(out + (FLAT ? 0 : at[k].row) * cols + (int64_t)at[k].unit * 8, cols - (int64_t)at[k].unit * 8, v);
     }
 }
 
@@ -106,6 +126,8 @@ using namespace gq;
 // Units a lane: 4 keep enough in flight in long launches, in short ones more lanes do (quantise 8192x8192 bf16: 47.1, 44.9 and 43.7 us
 // with 1, 2 and 4, unfold 35.1, 33.5, 32.0; 2048x4096: 8.1, 7.9, 9.4 and 5.8, 5.9, 6.7; 128x4096: 3.0, 3.8, 5.6 and 1.9, 2.1, 2.5).
 constexpr int64_t kLongWeights = 1 << 21;
+// rows of whole groups: codes and scales of a row end where the next one's begin, the matrix is one row
+static bool is_flat(int64_t rows, int64_t cols, int group) { return cols % group == 0 && flat_fits(rows * (cols / 8)); }
 static bool long_launch(int64_t units, int64_t cols) { return cols >= 8 && units >= kLongWeights; }
 
 extern "C" {
@@ -120,8 +142,11 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
     if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return GQ_OK;
     if (!aligned(w, 16) || !aligned(codes_out, 16) || !aligned(scales_out, 16)) return GQ_ERR_INVALID_ARG;
+    const bool flat = is_flat(rows, cols, group);
+    if (flat) cols *= rows, rows = 1;
     // whole groups of units, whole words of codes
-    const int64_t per_row = ((cols + group - 1) / group * group) / 8, units = rows * per_row, per_block = (int64_t)(long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
+    const int64_t row_words = (cols + 31) / 32 * 4, per_row = ((cols + group - 1) / group * group) / 8, units = rows * per_row;
+    const int64_t per_block = (long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
@@ -129,13 +154,15 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
             typedef decltype(s) S;
             auto of_group = [&](auto g) {
                 constexpr int GROUP = decltype(g)::value;
-                return cols < 8 ? group_quantize_kernel<T, S, GROUP, true, 1>
-                                : long_launch(units, cols) ? group_quantize_kernel<T, S, GROUP, false, 4> : group_quantize_kernel<T, S, GROUP, false, 1>;
+                const bool four = long_launch(units, cols);
+                return cols < 8 ? group_quantize_kernel<T, S, GROUP, true, false, 1>
+                       : flat ? (four ? group_quantize_kernel<T, S, GROUP, false, true, 4> : group_quantize_kernel<T, S, GROUP, false, true, 1>)
+                              : (four ? group_quantize_kernel<T, S, GROUP, false, false, 4> : group_quantize_kernel<T, S, GROUP, false, false, 1>);
             };
             auto kernel = group == 32 ? of_group(std::integral_constant<int, 32>())
                                       : group == 64 ? of_group(std::integral_constant<int, 64>()) : of_group(std::integral_constant<int, 128>());
             kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)w, rows, cols, (uint32_t)per_row, (int)((cols + group - 1) / group),
-                                                                           (uint32_t)(gq_w4_row_bytes(cols) / 4), (uint32_t *)codes_out, (S *)scales_out);
+                                                                           (uint32_t)row_words, (uint32_t *)codes_out, (S *)scales_out);
             return launched();
         });
     });
@@ -149,16 +176,21 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
     if (!float_type(dtype)) return GQ_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return GQ_OK;
     if (!aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, 16)) return GQ_ERR_INVALID_ARG;
-    const int64_t per_row = (cols + 7) / 8, units = rows * per_row, per_block = (int64_t)(long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
+    const bool flat = is_flat(rows, cols, group);
+    if (flat) cols *= rows, rows = 1;
+    const int64_t row_words = (cols + 31) / 32 * 4, per_row = (cols + 7) / 8, units = rows * per_row;
+    const int64_t per_block = (long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         return with_scale_type(scale_dtype, [&](auto s) {
             typedef decltype(s) S;
-            auto kernel = long_launch(units, cols) ? group_dequantize_kernel<T, S, 4> : group_dequantize_kernel<T, S, 1>;
+            const bool four = long_launch(units, cols);
+            auto kernel = flat ? (four ? group_dequantize_kernel<T, S, true, 4> : group_dequantize_kernel<T, S, true, 1>)
+                               : (four ? group_dequantize_kernel<T, S, false, 4> : group_dequantize_kernel<T, S, false, 1>);
             kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>(
                 (const uint32_t *)codes, (const S *)scales, rows, cols, (uint32_t)per_row, group == 32 ? 5 : group == 64 ? 6 : 7,
-                (int)((cols + group - 1) / group), (uint32_t)(gq_w4_row_bytes(cols) / 4), (T *)out);
+                (int)((cols + group - 1) / group), (uint32_t)row_words, (T *)out);
             return launched();
         });
     });

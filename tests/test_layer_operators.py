@@ -263,6 +263,40 @@ def test_dropout_of_a_matrix_cut_between_rows(n, bits):
     assert not torch.equal(whole, other)                             # another worker draws on its own
 
 
+@gpu
+@pytest.mark.parametrize("rows,n", [(4100, 4104), (4100, 4099), (1, 17_000_003)])
+def test_long_launches_equal_their_parts(rows, n):
+    """Dropout and 4-bit weights of more elements than a short launch has: whole rows against calls on some of them."""
+    x = torch.randn(rows, n, device=DEV, dtype=torch.bfloat16)
+    whole = torch.empty_like(x)
+    pitch = 8 * math.ceil(n / 8)
+    for bits in (32, 16):
+        gq.dropout(x, gq.make_dropout(0.4, 9, 1, 16, bits), whole, residual=x)
+        if rows == 1:                                                 # whole units: one row of the stream
+            for a, b in ((0, 8000), (8_000_000, 8_100_000), (17_000_000 - 8000, n)):
+                part = torch.empty(1, b - a, device=DEV, dtype=x.dtype)
+                gq.dropout(x[:, a:b].clone(), gq.make_dropout(0.4, 9, 1, 16 + a, bits), part, residual=x[:, a:b].clone())
+                assert torch.equal(part, whole[:, a:b])
+        else:
+            for a, b in ((0, 50), (2040, 2100), (rows - 30, rows)):
+                part = torch.empty(b - a, n, device=DEV, dtype=x.dtype)
+                gq.dropout(x[a:b].clone(), gq.make_dropout(0.4, 9, 1, 16 + pitch * a, bits), part, residual=x[a:b].clone())
+                assert torch.equal(part, whole[a:b])
+    if rows == 1:
+        return
+    for group in (32, 64, 128):
+        G, st = -(-n // group), torch.bfloat16
+        codes, scales = Guarded((rows, gq.w4_row_bytes(n)), torch.uint8), Guarded((rows, G), st)
+        gq.group_quantize(x, group, codes.t, scales.t)
+        gq.group_dequantize(codes.t, scales.t, group, whole)
+        for a, b in ((0, 50), (2040, 2100), (rows - 30, rows)):
+            pc, ps, pv = torch.empty(b - a, gq.w4_row_bytes(n), dtype=torch.uint8, device=DEV), torch.empty(b - a, G, dtype=st, device=DEV), torch.empty(b - a, n, device=DEV, dtype=x.dtype)
+            gq.group_quantize(x[a:b].clone(), group, pc, ps)
+            gq.group_dequantize(pc, ps, group, pv)
+            assert torch.equal(pc, codes.t[a:b]) and torch.equal(ps, scales.t[a:b]) and torch.equal(pv, whole[a:b])
+        assert codes.intact() and scales.intact()
+
+
 # ---- RMS norm -------------------------------------------------------------------------------------------------------
 
 NS = [1, 7, 8, 65, 512, 1000, 2047, 2048, 2049, 4096, 5003, 8192, 8193, 16384, 20001, 32768]
@@ -416,6 +450,29 @@ def test_rms_norm_backward(n, rows, name, weight):
         elif sd is not None:
             gq.rms_norm_backward(yd, hd, w.to(DEV), rstd.to(DEV), sd, dsum=sd, dweight_out=twice)
             assert torch.equal(sd, dx.t) and torch.equal(twice, dw.t)
+
+
+@gpu
+@pytest.mark.parametrize("draws", [0, 16, 32])
+@pytest.mark.parametrize("n", [5, 136, 900, 1500, 2500, 5003, 7001])
+def test_rms_norm_backward_of_many_rows(n, draws):
+    """More rows than a workgroup's first: each row alone against the same call on some of the rows, the weight's gradient against 64 bits."""
+    rows = 8300 if n < 1000 else 2101
+    g = torch.Generator().manual_seed(n)
+    dev = lambda v: v.to(DEV)                                         # noqa: E731
+    h, dy, ds, w = (dev(randn(g, *s, t=torch.bfloat16)) for s in ((rows, n), (rows, n), (rows, n), (n,)))
+    rstd = (1.0 / torch.sqrt(h.double().square().mean(1) + 1e-5)).float()
+    make = lambda first: gq.make_dropout(0.25, SEED, 2, 8 * math.ceil(n / 8) * first, draws) if draws else None     # noqa: E731
+    dx, dres, dw = torch.empty_like(h), torch.empty_like(h), torch.empty(n, device=DEV)
+    gq.rms_norm_backward(dy, h, w, rstd, dx, dsum=ds, dres_out=dres if draws else None, dweight_out=dw, drop=make(0))
+    for a, b in ((0, 100), (700, 1100), (rows - 61, rows)):
+        px, pres = torch.empty(b - a, n, dtype=h.dtype, device=DEV), torch.empty(b - a, n, dtype=h.dtype, device=DEV)
+        cut = [v[a:b].clone() for v in (dy, h, ds, rstd)]
+        gq.rms_norm_backward(cut[0], cut[1], w, cut[3], px, dsum=cut[2], dres_out=pres if draws else None, drop=make(a))
+        assert torch.equal(px, dx[a:b]) and (not draws or torch.equal(pres, dres[a:b]))
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    # 512 or 256 parts of at most rows / 256 + 1 terms in turn, then 16 slices of 32 parts: that many roundings at most
+    close(dw, terms.sum(0), (rows // 256 + 2 + 32 + 16 + 3) * U * terms.abs().sum(0))
 
 
 @gpu
@@ -602,6 +659,27 @@ def test_w4_matvec_rows_are_apart(x_type):
     bad = torch.zeros(20, 50, dtype=torch.bool, device=DEV)
     bad[3], bad[7], bad[18], bad[:, 11] = True, True, True, True
     assert torch.equal(torch.isnan(y), bad) and torch.equal(y[~bad], clean[~bad])
+
+
+# every shape of workgroup that the rule chooses from: few and many rows of x, from a few rows of weights to over 16384
+@gpu
+@pytest.mark.parametrize("x_type,out,scale,group", [("bf16", "f32", "bf16", 128), ("f16", "f16", "f32", 64), ("i8", "f32", "bf16", 32)])
+@pytest.mark.parametrize("m,rows,cols", [(1, 9001, 260), (2, 12000, 2100), (3, 9001, 260), (8, 17001, 136), (8, 40, 9001), (12, 5000, 1100), (12, 9001, 260),
+                                         (12, 12000, 136), (12, 17001, 136), (30, 5000, 600), (30, 9001, 260), (30, 12000, 136), (30, 17001, 136),
+                                         (50, 5000, 600), (50, 9001, 260), (50, 12000, 136), (50, 17001, 136), (100, 9001, 136)])
+def test_w4_matvec_of_many_rows(m, rows, cols, group, x_type, out, scale):
+    g = torch.Generator().manual_seed(m * 7919 + rows * 31 + cols + group)
+    q, codes, scales = weights(g, rows, cols, group, TYPES[scale])
+    if x_type == "i8":
+        x, xs = torch.randint(-128, 128, (m, cols), generator=g).to(torch.int8), 0.01 + torch.rand(m, generator=g)
+    else:
+        x, xs = randn(g, m, cols, std=0.1, t=TYPES[x_type]), None
+    t = TYPES[out]
+    y = Guarded((m, rows), t)
+    gq.w4_matvec(x.to(DEV), codes, scales, group, y.t, x_scales=None if xs is None else xs.to(DEV))
+    want, tol = plain_matvec(x, xs, q, scales, group, None)
+    close(y.t, want, tol + half_step(t) * (want.abs() + tol) + least(t))
+    assert y.intact()
 
 
 @gpu
