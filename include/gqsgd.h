@@ -362,7 +362,7 @@ gq_status gq_dropout(const void *x, const void *residual, int64_t rows, int64_t 
  *   sum_out        device [rows][n] of `dtype`: h, or NULL; may be x or residual
  *   out            device [rows][n] of out_dtype; may be x or residual where out_dtype is `dtype`, not sum_out
  *   out_dtype      `dtype`, or GQ_I8 / GQ_E4M3: 8 bits under a scale per row.  With a = max |y| of the row and top = 127 or 448,
- *                  scale = fl32(a / top) and the code is y fl32(1 / scale) rounded to nearest even.  A row of zeros, and one
+ *                  scale = fl32(a fl32(1 / top)) and the code is y fl32(1 / scale) rounded to nearest even.  A row of zeros, and one
  *                  whose 1 / scale is not finite, has scale 0 and codes 0; a row that is not finite has scale NaN and codes 0.
  *   scales_out     device fp32[rows] for the 8-bit types, else NULL
  *   rstd_out       device fp32[rows], or NULL: what the backward pass takes */
@@ -392,7 +392,7 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
  * each `group` consecutive columns of a row (the last group may be short): scales [rows][ceil(cols/group)] of GQ_F32 or
  * GQ_BF16.  group is 32, 64 or 128.  Column c of a row stands for code times the scale of group c / group.
  *
- * gq_group_quantize: with a = max |w| of the group, scale = fl32(a / 7) rounded to scale_dtype; the code is w / scale rounded to
+ * gq_group_quantize: with a = max |w| of the group, scale = fl32(a fl32(1 / 7)) rounded to scale_dtype; the code is w / scale rounded to
  * nearest, ties to even (the exact quotient), -7 .. 7.  A group of zeros, and one whose 1 / scale is not finite in binary32, has
  * scale 0 and codes 0; a group that is not finite has scale NaN and codes 0.
  *   w           device [rows][cols] of `dtype` (GQ_F32, GQ_BF16, GQ_F16)

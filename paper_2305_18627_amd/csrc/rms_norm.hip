@@ -52,12 +52,12 @@ __device__ __forceinline__ float reciprocal_root(double v)
 }
 
 struct RowScale { float scale, inv; };
-// scale and what codes are multiplied by, for a row whose largest magnitude has the bits `top_bits`
-__device__ __forceinline__ RowScale row_scale(uint32_t top_bits, float top)
+// scale and what codes are multiplied by, for a row whose largest magnitude has the bits `top_bits`; per_top: 1 / the largest code
+__device__ __forceinline__ RowScale row_scale(uint32_t top_bits, float per_top)
 {
     const float a = __uint_as_float(top_bits);
     if (top_bits >= 0x7F800000u) return {__builtin_nanf(""), 0.0f};
-    const float scale = a / top, inv = 1.0f / scale;
+    const float scale = a * per_top, inv = 1.0f / scale;
     if (!(inv <= 3.402823466e+38f)) return {0.0f, 0.0f};              // a row of zeros, or too small to be scaled
     return {scale, inv};
 }
@@ -144,7 +144,7 @@ rms_norm_kernel(NormArgs p)
 #pragma unroll
         for (int i = 0; i < 8; i++) m = max(m, 8 * (lane + k * kLanes) + i < p.n ? __float_as_uint(h[k][i]) & 0x7FFFFFFFu : 0u);
     const float top = p.out_dtype == GQ_I8 ? 127.0f : 448.0f;
-    const RowScale rs = row_scale(team_max<WPR>(m, tops), top);
+    const RowScale rs = row_scale(team_max<WPR>(m, tops), p.out_dtype == GQ_I8 ? 1.0f / 127.0f : 1.0f / 448.0f);
     if (lane == 0) p.scales_out[row] = rs.scale;
 #pragma unroll
     for (int k = 0; k < STEPS; k++) {

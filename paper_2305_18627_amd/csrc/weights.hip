@@ -25,12 +25,7 @@ template <typename S> struct GroupScale { S stored; float scale, inv; };
 template <typename S> __device__ __forceinline__ GroupScale<S> group_scale(uint32_t top_bits)
 {
     if (top_bits >= 0x7F800000u) return {(S)__builtin_nanf(""), 0.0f, 0.0f};
-    // a / 7: a times the rounded 1/7 and one correction is the correctly rounded quotient (verified over all 2^23 mantissas), far
-    // enough from the smallest numbers; there, the division itself
-    const float a = __uint_as_float(top_bits), sevenths = 1.0f / 7.0f;
-    const float q0 = a * sevenths;
-    const float seventh = a >= 0x1p-90f ? __builtin_fmaf(__builtin_fmaf(-7.0f, q0, a), sevenths, q0) : a / 7.0f;
-    const S stored = (S)seventh;
+    const S stored = (S)(__uint_as_float(top_bits) * (1.0f / 7.0f));
     const float scale = (float)stored;
     if (!(scale > 0x1p-128f)) return {(S)0.0f, 0.0f, 0.0f};                   // 1 / scale is not finite
     return {stored, scale, scale >= 0x1p-120f ? __builtin_amdgcn_rcpf(scale) : 1.0f / scale};   // an ulp does not matter to the codes

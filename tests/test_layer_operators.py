@@ -547,7 +547,7 @@ def test_group_quantize_and_dequantize(cols, group, name, scale):
     gq.group_dequantize(codes.t, scales.t, group, out.t)
     assert codes.intact() and scales.intact() and out.intact()
     padded = torch.nn.functional.pad(w, (0, G * group - cols)).reshape(rows, G, group)
-    want = (padded.float().abs().amax(2) / 7.0).to(st)                # one division in binary32 and one rounding: the same bits
+    want = (padded.float().abs().amax(2) * torch.tensor(1.0 / 7.0)).to(st)     # one product in binary32 and one rounding: the same bits
     assert torch.equal(scales.t.cpu(), want)
     s = per_column(want, cols, group)
     quotient = torch.where(s > 0, w.double() / s, 0.0)                # 24-bit numbers: nearest and ties come out right in 64 bits
