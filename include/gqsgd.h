@@ -319,8 +319,10 @@ gq_status gq_sparse_aggregate(const uint32_t *const *indices /* host */, const i
  *
  * Matrices are dense and row-major; their first element is 16-byte aligned, their rows need not be (any row length).
  * Every call is defined for 0 rows and 0 columns (nothing is written but the sums that are empty).  Sums, norms and scales
- * are formed in binary32 or wider and a result is rounded once, to nearest even, to the type that it is stored in.
- * Sizes that one launch cannot cover (about 2^35 elements) are answered with GQ_ERR_INVALID_ARG.
+ * are formed in binary32 or wider and a result is rounded once, to nearest even, to the type that it is stored in.  An output
+ * shares no memory with anything else of its call, but for the whole matrices that are said to be allowed.
+ * Sizes that one launch cannot cover are answered with GQ_ERR_INVALID_ARG: about 2^35 elements, and fewer where rows are short
+ * (a norm of up to 1024 columns takes fewer than 2^26 rows, of up to 8192 fewer than 2^24).
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef enum {
     GQ_F32 = 0,    /* binary32                                              */
@@ -390,7 +392,7 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
 /* 4-bit weights under group scales.  A matrix [rows][cols] is stored as codes -7 .. 7 of the linear grid (s = 7) in the
  * nibbles of GQ_PACK_I4, every row padded with zero codes to gq_w4_row_bytes(cols) = 16 ceil(cols/32) bytes, and one scale for
  * each `group` consecutive columns of a row (the last group may be short): scales [rows][ceil(cols/group)] of GQ_F32 or
- * GQ_BF16.  group is 32, 64 or 128.  Column c of a row stands for code times the scale of group c / group.
+ * GQ_BF16.  group is 32, 64 or 128; rows <= 2^30, cols <= 2^24.  Column c of a row stands for code times the scale of group c / group.
  *
  * gq_group_quantize: with a = max |w| of the group, scale = fl32(a fl32(1 / 7)) rounded to scale_dtype; the code is w / scale rounded to
  * nearest, ties to even (the exact quotient), -7 .. 7.  A group of zeros, and one whose 1 / scale is not finite in binary32, has
@@ -406,14 +408,16 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
                               void *out, gq_dtype dtype, void *hip_stream);
 
 /* Rows of activations times 4-bit weights: y[i][r] = x_scales[i] * sum over groups g of scale[r][g] * (sum over c in g of
- * code[r][c] x[i][c]) + bias[r].  Meant for few rows (m from 1 to some tens, the weights are read once for 64 of them); any m works.
+ * code[r][c] x[i][c]) + bias[r].  Meant for few rows (m from 1 to some tens: the weights are read again for every 32 or 64 of
+ * them); m <= 2^20, rows <= 2^30, cols <= 2^24.
  *   x         device [m][cols] of x_dtype: GQ_BF16, GQ_F16, or GQ_I8 (codes, as gq_rms_norm writes them)
  *   x_scales  device fp32[m] with GQ_I8, else NULL
  *   bias      device [rows] of y_dtype, or NULL
  *   y         device [m][rows] of y_dtype: GQ_F32, GQ_BF16 or GQ_F16
  * Products of int8 activations are summed exactly within a group.  Sums of GQ_BF16 and GQ_F16 activations are formed with the
  * codes moved by 24 (matrix instructions take 24 + code) and corrected by 24 times the sum of x: in binary32, so exact to a few
- * 2^-24 of 24 sum |x| over up to 128 columns.  A row of x that holds an infinity or a NaN gives NaN. */
+ * 2^-24 of 24 sum |x| over up to 128 columns.  A row of x that holds an infinity or a NaN gives NaN, and so may finite ones of
+ * which 31 times a group's sum of |x| leaves binary32. */
 gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t m, gq_dtype x_dtype, const void *codes, const void *scales,
                        gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, const void *bias, void *y, gq_dtype y_dtype,
                        void *hip_stream);

@@ -21,7 +21,7 @@ extern "C" gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t 
     const gq_status st = check_weights(rows, cols, group, scale_dtype);
     if (st != GQ_OK) return st;
     if ((x_dtype != GQ_BF16 && x_dtype != GQ_F16 && x_dtype != GQ_I8) || !float_type(y_dtype) || (x_dtype == GQ_I8) != (x_scales != nullptr) ||
-        !matrix_fits(m, cols) || !matrix_fits(m, rows)) return GQ_ERR_INVALID_ARG;
+        m > (1 << 20) || !matrix_fits(m, cols) || !matrix_fits(m, rows)) return GQ_ERR_INVALID_ARG;
     if (m == 0 || rows == 0) return GQ_OK;
     if (!aligned(y, 16) || !aligned_or_null(bias, 16) || (cols > 0 && (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16))) ||
         !aligned_or_null(x_scales, 4)) return GQ_ERR_INVALID_ARG;

@@ -398,7 +398,7 @@ static gq_status launch_matvec(const MatvecArgs &p, hipStream_t stream)
         lds = 2 * MT * 16 * kStep * (int)sizeof(X);
         if (lds < kParts) lds = kParts;
     }
-    if (!grid_fits(bx, 64 * WN * WK) || by > 65535) return GQ_ERR_INVALID_ARG;
+    if (!grid_fits(bx, 64 * WN * WK)) return GQ_ERR_INVALID_ARG;
     w4_matvec_kernel<X, S, GROUP, MT, WN, WK, U, RESIDENT><<<dim3((unsigned)bx, (unsigned)by), 64 * WN * WK, lds, stream>>>(p);
     return launched();
 }

@@ -468,6 +468,7 @@ gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t
     if (rows == 0 || n == 0) return GQ_OK;
     if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(out, 16) || !aligned_or_null(residual, 16) || !aligned_or_null(sum_out, 16) ||
         !aligned_or_null(scales_out, 4) || !aligned_or_null(rstd_out, 4) || out == sum_out) return GQ_ERR_INVALID_ARG;
+    if (bytes && (out == x || out == residual)) return GQ_ERR_INVALID_ARG;         // rows of codes lie over other rows of the input
     const NormArgs p = {x, residual, weight, sum_out, out, scales_out, rstd_out, rows, (int)n, (int)(pitch8(n) / 8), 1.0 / (double)n, (double)eps,
                         draw_bits(drop), (int)out_dtype, drop ? make_drop(drop) : Drop{}};
     return with_types(dtype, weight_dtype, [&](auto t, auto w) {

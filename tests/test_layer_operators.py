@@ -114,6 +114,7 @@ def test_refusals_of_the_c_abi_need_no_device():
     assert norm(ot=3) == I and norm(ot=4) == I and norm(sc=ok) == I                        # scales with 8 bits, and only then
     assert norm(x=odd) == I and norm(w=odd) == I and norm(out=odd) == I and norm(res=odd) == I and norm(s=odd) == I
     assert norm(s=C.c_void_p(0x2000)) == I                                                 # sum and out in one place
+    assert norm(ot=3, sc=ok, out=ok) == I and norm(ot=4, sc=ok, res=C.c_void_p(0x2000)) == I     # 8 bits over 16
     assert norm(rstd=C.c_void_p(0x1002)) == I and norm(ot=3, sc=C.c_void_p(0x1002)) == I
     assert norm(d=D(1.5, 1)) == I and norm(rows=-1) == I
     assert norm(n=gq.GQ_RMS_NORM_MAX_N + 1) == gq.GQ_ERR_UNSUPPORTED
@@ -143,7 +144,8 @@ def test_refusals_of_the_c_abi_need_no_device():
         return lib.gq_w4_matvec(x, xs, m, xt, c, s, st, rows, cols, g, b, y, yt, None)
     assert mv(xt=0) == I and mv(xt=4) == I and mv(yt=3) == I and mv(xt=3) == I and mv(xs=ok) == I and mv(g=48) == I and mv(st=2) == I
     assert mv(x=odd) == I and mv(c=odd) == I and mv(s=odd) == I and mv(y=odd) == I and mv(b=odd) == I and mv(xt=3, xs=C.c_void_p(0x1002)) == I
-    assert mv(m=-1) == I and mv(rows=-1) == I and mv(cols=-1) == I and mv(m=1 << 31) == I
+    assert mv(m=-1) == I and mv(rows=-1) == I and mv(cols=-1) == I and mv(m=1 << 31) == I and mv(m=(1 << 20) + 1) == I
+    assert mv(rows=(1 << 30) + 1) == I and mv(cols=(1 << 24) + 1) == I
     assert mv(m=0) == gq.GQ_OK and mv(rows=0) == gq.GQ_OK
 
 
