@@ -292,8 +292,8 @@ w4_matvec_kernel(MatvecArgs p)
         }
     };
 
-    Fetched now, next;
     if constexpr (RESIDENT) {
+        Fetched now, next;
         // the first units of x are asked for before the codes: loads come back in order, and x is wanted first
         const int units = m_rows << shift;
         constexpr int kFirst = 2;
@@ -333,14 +333,15 @@ w4_matvec_kernel(MatvecArgs p)
         static_assert(kThreads % kRowUnits == 0 && kAhead * kRowsApart == MT * 16, "units of a step");
         const int unit = threadIdx.x % kRowUnits, row0 = threadIdx.x / kRowUnits;
         Raw ahead[kAhead];
+        // rows of fewer than eight columns are read in put(); what is asked for here is then 16 bytes of codes, not used
+        const X *asked = p.cols < 8 ? (const X *)p.codes : x;
+        const int apart = p.cols < 8 ? 0 : p.cols;
         // a unit that runs over the row's end (or lies past it) is read so that it ends there, and moved into place in put()
         auto ask = [&](int step) {
-            const int c = min(step * kStep + 8 * unit, p.cols - 8);
-            if (p.cols >= 8) {
+            const int c = p.cols < 8 ? 0 : min(step * kStep + 8 * unit, p.cols - 8);
 #pragma unroll
-                for (int i = 0; i < kAhead; i++)
-                    __builtin_memcpy(&ahead[i], x + (uint32_t)(min(row0 + i * kRowsApart, m_rows - 1) * p.cols + c), sizeof(Raw));
-            }
+            for (int i = 0; i < kAhead; i++)
+                __builtin_memcpy(&ahead[i], asked + (uint32_t)(min(row0 + i * kRowsApart, m_rows - 1) * apart + c), sizeof(Raw));
         };
         auto put = [&](int step) {
             uint8_t *to = lds + (step & 1) * kBuffer;
@@ -357,23 +358,31 @@ w4_matvec_kernel(MatvecArgs p)
 #pragma unroll
             for (int i = 0; i < kAhead; i++) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
         };
+        // Codes are asked for two steps ahead, x one.  No branch is around a load, for what is loaded on one way only is waited for where the
+        // ways join: past the last step its loads come again.  us before and after both: 61 rows of x, 14335x4095, groups of 32, f16 34.3
+        // and 29.8; 64 rows, 8192x8192 29.7, 26.9, 28672x8192 75, 68; 64x14000 33.7, 28.3.  Three sets of codes only as far as 128
+        // registers reach (else they spill: 32 rows, 4096x4096, groups of 32 9.0 and 13.4), and not for 16 rows in int8 (12.6, 13.7).
+        constexpr int kWords = 3 * (4 * U + kScaleWords) + kAhead * (int)sizeof(Raw) / 4;
+        constexpr int kSets = MT <= 2 && sizeof(X) * MT >= 2 && kWords <= 45 ? 3 : 2;
+        Fetched f[kSets];
         clear();
         if (steps > 0) {
             ask(0);
-            fetch(blockIdx.x, 0, now);
+#pragma unroll
+            for (int k = 0; k + 1 < kSets; k++) fetch(blockIdx.x, min(k, steps - 1), f[k]);
             put(0);
         }
         __syncthreads();
-        for (int step = 0; step < steps; step++) {
-            const bool more = step + 1 < steps;
-            if (more) {
-                ask(step + 1);
-                fetch(blockIdx.x, step + 1, next);
+        for (int step = 0; step < steps;) {
+#pragma unroll
+            for (int k = 0; k < kSets; k++) {
+                ask(min(step + 1, steps - 1));
+                fetch(blockIdx.x, min(step + kSets - 1, steps - 1), f[(k + kSets - 1) % kSets]);
+                multiply(f[k], step, lds + (step & 1) * kBuffer);
+                if (step + 1 < steps) put(step + 1);         // last read two steps ago, before the barrier that ended that step
+                __syncthreads();
+                if (++step >= steps) break;
             }
-            multiply(now, step, lds + (step & 1) * kBuffer);
-            if (more) put(step + 1);                     // last read two steps ago, before the barrier that ended that step
-            now = next;
-            __syncthreads();
         }
         float *part = reinterpret_cast<float *>(lds);
         leave(part);
@@ -414,6 +423,7 @@ static gq_status launch_matvec(const MatvecArgs &p, hipStream_t stream)
 //   8192x8192   32: 17.5, 64: 24.4, 16: 24.7       |  slices of 16, 64: 24.2, of 32, 32: 25.2, 64: 29.4 |  slices of 32, 64: 30.0, 32: 45.8
 //   14336x4096  64: 14.2, 32: 15.5                 |  64: 17.0, 32: 19.6                                |  slices of 32, 128: 26.0, of 64, 64: 26.8
 //   28672x8192  64 (8 waves): 38.2, 128: 46.3, 64 (16 waves): 48.5  |  64 (8 waves): 50.1, 128: 51.7    |  128: 72.3, slices of 32, 128: 93.7
+// (taken with codes one step ahead; the first of each now: 6.3, 8.9, 12.3; 16.8, 22.8, 26.9; 13.7, 17.0, 23.7; 39.8, 51.5, 68)
 template <typename X, typename S, int GROUP> static gq_status matvec_of_group(MatvecArgs p, hipStream_t stream)
 {
     const int64_t tiles = (p.rows + 15) / 16;
