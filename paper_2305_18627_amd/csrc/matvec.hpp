@@ -99,6 +99,10 @@ struct MatvecArgs {
     int row_shift;        // a row of staged x in LDS has 2^row_shift columns
 };
 
+// y = x times the transposed weights: 2 m rows cols operations on rows cols / 2 bytes of codes, which are read once for all rows of x of a
+// slice.  Bound by these bytes for a row or a few (28672x8192, int8, 132 MB with scales: 28-29 us, 4.6 TB/s; a bare read of such codes
+// takes 22); for more rows by what a step costs beside them: x through LDS, unfolding, the barrier (61 rows, 14335x4095: 28.5 us, 250
+// TFLOP/s); for small matrices by latency (4096x4096: 4.2-5 us).
 // A workgroup of WN x WK waves owns WN * 16 rows of the weights at a time and up to MT * 16 rows of x; the WK waves share out
 // the columns, 128 U at a time (a step), and their sums are joined in LDS at a tile's end.  x is staged in LDS: RESIDENT, all of
 // it, once, for all tiles of rows that the workgroup takes in turn; otherwise a step's columns at a time into two buffers in

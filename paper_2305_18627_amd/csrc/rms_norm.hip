@@ -9,19 +9,20 @@
 
 namespace gq {
 
+// h = residual + dropout(x), y = h rstd weight, rstd = 1 / sqrt(mean(h^2) + eps): a sum over the row and a second look at it.
 // A row belongs to a team of WPR waves, whose lanes hold STEPS units of eight columns each, 64 WPR units apart, from the first
 // load to the last store: a row is read once.  Teams of one wave share a workgroup of four.
 template <int WPR> constexpr int kTeams = WPR == 1 ? 4 : 1;
 template <int WPR> constexpr int kThreads = 64 * WPR * kTeams<WPR>;
 
-// the sum over a team, the same for all its lanes; `lds` is not used again before the workgroup's next barrier but one
-template <int WPR> __device__ __forceinline__ double team_sum(double v, double *lds)
+// the sum over a team, the same for all its lanes; `lds`, the team's own, is not used again before the workgroup's next barrier but one
+template <int WPR, int TEAMS = 1> __device__ __forceinline__ double team_sum(double v, double *lds)
 {
     v = wave_sum(v);
     if constexpr (WPR == 1) {
         return v;
     } else {
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) lds[TEAMS > 1 ? (threadIdx.x >> 6) % WPR : threadIdx.x >> 6] = v;
         __syncthreads();
         double s = 0.0;
 #pragma unroll
@@ -79,6 +80,8 @@ struct NormArgs {
     Drop drop;
 };
 
+// Bound by memory in long launches: 8192x4096 bf16 with a residual and dropout, sum and y written, 45 us, 6.0 TB/s; fp32 without dropout
+// 98 us, 5.5 TB/s.  By latency (the load, the sum's round through the team, the 8-bit maximum's) in short ones: 1x4096 3.2 us.
 template <typename T, typename W, int WPR, int STEPS, bool TINY, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads<WPR>)
 rms_norm_kernel(NormArgs p)
@@ -199,16 +202,20 @@ template <typename T> __device__ __forceinline__ void forget(Eight<T> &t)
     }
 }
 
+// dh = dsum + rstd (g - xh mean(g xh)) and dweight = sum over rows of dy xh, with xh = h rstd, g = dy weight: one pass over the rows.
 // A workgroup takes rows (its teams one each) in turn, gridDim.x * teams apart, and keeps the weight's gradient of its columns in
 // registers; its sums go to `parts` and a second kernel adds those up.  AHEAD: the next row is asked for before the current one is
-// reduced, where the registers reach.
-template <typename T, typename W, int WPR, int STEPS, bool TINY, bool DSUM, bool AHEAD>
-__global__ void __launch_bounds__(kThreads<WPR>)
+// reduced, where the registers reach.  dweight stays in binary32: a lane adds up no more than its workgroup's share of the rows.
+// Bound by memory: 8192x4096 bf16 with dsum and dropout 61 us, 5.5 TB/s, and 4.8 us for the parts' sum; 1000x2047 fp32, four rows a
+// workgroup one after another, 8.4 and 2.5 us.
+template <typename T, typename W, int WPR, int STEPS, int TEAMS, bool TINY, bool DSUM, bool AHEAD>
+__global__ void __launch_bounds__(64 * WPR * TEAMS)
 rms_norm_backward_kernel(BackwardArgs p)
 {
-    constexpr int kLanes = 64 * WPR, kTeam = kTeams<WPR>;
-    __shared__ double sums[2][WPR];
-    __shared__ float joined[kTeam > 1 ? kTeam - 1 : 1][kTeam > 1 ? STEPS * 512 : 1];
+    constexpr int kLanes = 64 * WPR, kTeam = TEAMS;
+    constexpr bool kTogether = TEAMS > 1 && WPR > 1;                  // there is a barrier in each turn, and several teams at it
+    __shared__ double sums[2][kTeam][WPR];
+    __shared__ float joined[kTeam > 1 ? kTeam - 1 : 1][kTeam > 1 ? STEPS * 8 * kLanes : 1];
     const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
     const int64_t stride = (int64_t)gridDim.x * kTeam;
     struct Row { Eight<T> dy[STEPS], h[STEPS], ds[DSUM ? STEPS : 1]; float rstd; };
@@ -234,13 +241,15 @@ rms_norm_backward_kernel(BackwardArgs p)
     }
     int64_t row = (int64_t)blockIdx.x * kTeam + team;
     if (AHEAD && row < p.rows) fetch(row, now);
-    for (int turn = 0; row < p.rows; row += stride, turn ^= 1) {
-        if (!AHEAD) fetch(row, now);
+    // at a barrier as many turns for each team: one without a row only takes part in that
+    for (int turn = 0; (kTogether ? row - team : row) < p.rows; row += stride, turn ^= 1) {
+        const bool live = !kTogether || row < p.rows;
+        if (!AHEAD && live) fetch(row, now);
         if (AHEAD && row + stride < p.rows) fetch(row + stride, next);
         const float rstd = now.rstd;
         double s = 0.0;
 #pragma unroll
-        for (int k = 0; k < STEPS; k++) {
+        for (int k = 0; k < STEPS && live; k++) {
             settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.dy[k]);
             settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.h[k]);
             if (DSUM) settle8<TINY>(p.n, 8 * (lane + k * kLanes), now.ds[k]);
@@ -252,9 +261,9 @@ rms_norm_backward_kernel(BackwardArgs p)
             }
             __builtin_amdgcn_sched_barrier(0);                        // a unit after another: all at once hold too many registers
         }
-        const float mean = (float)(team_sum<WPR>(s, sums[turn]) * p.per_n);
+        const float mean = (float)(team_sum<WPR, kTeam>(s, sums[turn][team]) * p.per_n);
 #pragma unroll
-        for (int k = 0; k < STEPS; k++) {
+        for (int k = 0; k < STEPS && live; k++) {
             const int u = lane + k * kLanes, left = p.n - 8 * u;
             const int64_t at = row * p.n + 8 * u;
             forget(now.dy[k]);
@@ -281,7 +290,7 @@ rms_norm_backward_kernel(BackwardArgs p)
 #pragma unroll
             for (int k = 0; k < STEPS; k++)
 #pragma unroll
-                for (int i = 0; i < 8; i++) joined[team - 1][(k * 8 + i) * 64 + lane] = dw[k][i];
+                for (int i = 0; i < 8; i++) joined[team - 1][(k * 8 + i) * kLanes + lane] = dw[k][i];
         }
         __syncthreads();
         if (team > 0) return;
@@ -290,7 +299,7 @@ rms_norm_backward_kernel(BackwardArgs p)
 #pragma unroll
             for (int k = 0; k < STEPS; k++)
 #pragma unroll
-                for (int i = 0; i < 8; i++) dw[k][i] += joined[t][(k * 8 + i) * 64 + lane];
+                for (int i = 0; i < 8; i++) dw[k][i] += joined[t][(k * 8 + i) * kLanes + lane];
     }
     float *part = p.parts + (int64_t)blockIdx.x * p.units * 8;
 #pragma unroll
@@ -303,7 +312,8 @@ rms_norm_backward_kernel(BackwardArgs p)
     }
 }
 
-// The same for rows that the registers of a team do not hold: each is read twice, the weight's gradient is kept in LDS.
+// The same for rows that the registers of a team do not hold: each is read twice, the weight's gradient is kept in LDS.  The second
+// reading and the round through LDS bound it: 1024x32768 bf16 with dsum 75 us, 3.6 TB/s of the bytes that one reading moves.
 constexpr int kLongBlock = 1024;
 template <typename T, typename W>
 __global__ void __launch_bounds__(kLongBlock)
@@ -371,24 +381,26 @@ rms_norm_backward_long_kernel(BackwardArgs p)
     }
 }
 
-// A workgroup adds up `count` parts of 64 columns: 16 lanes of four columns, 16 slices of the parts, joined in a fixed order.
+// A workgroup adds up `count` parts of kSumColumns columns: a lane four columns of a slice of the parts, joined in a fixed order.
+// 32: 2048x2048 12.5 us with the whole backward pass, 64: 13.0, 16: 13.4; 1000x2047 13.7, 14.1, 12.7
+constexpr int kSumColumns = 32, kSumLanes = kSumColumns / 4, kSlices = 256 / kSumLanes;
 __global__ void __launch_bounds__(256)
 weight_sum_kernel(const float *parts, int count, int n, int pitch, float *dweight)
 {
-    __shared__ f32x4 slices[16][16];
-    const int c4 = threadIdx.x % 16, slice = threadIdx.x / 16, c = blockIdx.x * 64 + 4 * c4;
+    __shared__ f32x4 slices[kSlices][kSumLanes];
+    const int c4 = threadIdx.x % kSumLanes, slice = threadIdx.x / kSumLanes, c = blockIdx.x * kSumColumns + 4 * c4;
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < pitch) {
 #pragma unroll 8
-        for (int i = slice; i < count; i += 16) s += *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * pitch + c);
+        for (int i = slice; i < count; i += kSlices) s += *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * pitch + c);
     }
     slices[slice][c4] = s;
     __syncthreads();
-    const int column = blockIdx.x * 64 + threadIdx.x;
-    if (threadIdx.x >= 64 || column >= n) return;
+    const int column = blockIdx.x * kSumColumns + threadIdx.x;
+    if (threadIdx.x >= kSumColumns || column >= n) return;
     float t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; i++) t += slices[i][threadIdx.x / 4][threadIdx.x % 4];
+    for (int i = 0; i < kSlices; i++) t += slices[i][threadIdx.x / 4][threadIdx.x % 4];
     dweight[column] = t;
 }
 
@@ -408,12 +420,17 @@ template <typename F> static gq_status with_types(int dtype, int weight_dtype, F
     });
 }
 
-// f(waves per row, steps, fewer than eight columns) of the smallest team that holds a row of n columns, as compile-time constants
-template <typename F> static gq_status with_team(int64_t n, F &&f)
+// f(waves per row, steps, fewer than eight columns) of the smallest team that holds a row of n columns, as compile-time constants.  Of
+// up to kFewRows rows, less than what a unit's latency covers, with one step a lane: 61x5003 fp16 to 8 bits 4.8 and 4.7 us, 1x4096
+// 2.9, 2.7, 64x8192 fp32 with dropout 5.9, 4.8, 256x8192 bf16 4.7, 4.7; 8192 rows of 4096 columns have one of 4 waves (45 us).
+constexpr int64_t kFewRows = 256;
+template <typename F> static gq_status with_team(int64_t rows, int64_t n, F &&f)
 {
     using std::integral_constant;
     const std::false_type no;
     if (n < 8) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), std::true_type());
+    if (rows <= kFewRows && n > 2048 && n <= 4096) return f(integral_constant<int, 8>(), integral_constant<int, 1>(), no);
+    if (rows <= kFewRows && n > 4096 && n <= 8192) return f(integral_constant<int, 16>(), integral_constant<int, 1>(), no);
     if (n <= 512) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), no);
     if (n <= 1024) return f(integral_constant<int, 1>(), integral_constant<int, 2>(), no);
     if (n <= 2048) return f(integral_constant<int, 4>(), integral_constant<int, 1>(), no);
@@ -424,29 +441,37 @@ template <typename F> static gq_status with_team(int64_t n, F &&f)
     return f(integral_constant<int, 16>(), integral_constant<int, 4>(), no);
 }
 
-// The same for the backward pass, whose rows come with twice the registers; none for rows of more than 16384 columns.
-template <typename F> static gq_status with_backward_team(int64_t n, F &&f)
+constexpr int64_t kManyRows = 2048;
+static bool four_teams(int64_t rows, int64_t n) { return n > 1024 && n <= 2048 && rows >= kManyRows; }
+
+// f(waves per row, steps, teams a workgroup, fewer than eight columns) for the backward pass, whose rows come with twice the registers;
+// none for rows of more than 16384 columns.  Teams of four waves: one a workgroup for few rows, four, with one part of the weight's
+// gradient between them, for many.  us with one and four: 300x2047 bf16 7.7, 8.5; 1000x2047 fp32 11.1, 13.7;
+// 1500x2047 13.5, 15.6, 2048x2047 17.3, 17.6; bf16 4096x2047 22.8, 18.4; with dropout 2048x2048 15.9, 12.5, 16384x2048 70.5, 61.3.
+template <typename F> static gq_status with_backward_team(int64_t rows, int64_t n, F &&f)
 {
     using std::integral_constant;
     const std::false_type no;
-    if (n < 8) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), std::true_type());
-    if (n <= 512) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), no);
-    if (n <= 1024) return f(integral_constant<int, 1>(), integral_constant<int, 2>(), no);
-    if (n <= 2048) return f(integral_constant<int, 4>(), integral_constant<int, 1>(), no);
-    if (n <= 4096) return f(integral_constant<int, 8>(), integral_constant<int, 1>(), no);
-    if (n <= 6144) return f(integral_constant<int, 12>(), integral_constant<int, 1>(), no);
-    if (n <= 8192) return f(integral_constant<int, 8>(), integral_constant<int, 2>(), no);
-    return f(integral_constant<int, 16>(), integral_constant<int, 2>(), no);
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 4> four;
+    if (n < 8) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), four, std::true_type());
+    if (n <= 512) return f(integral_constant<int, 1>(), integral_constant<int, 1>(), four, no);
+    if (n <= 1024) return f(integral_constant<int, 1>(), integral_constant<int, 2>(), four, no);
+    if (n <= 2048) return four_teams(rows, n) ? f(four, one, four, no) : f(four, one, one, no);
+    if (n <= 4096) return f(integral_constant<int, 8>(), integral_constant<int, 1>(), one, no);
+    if (n <= 6144) return f(integral_constant<int, 12>(), integral_constant<int, 1>(), one, no);
+    if (n <= 8192) return f(integral_constant<int, 8>(), integral_constant<int, 2>(), one, no);
+    return f(integral_constant<int, 16>(), integral_constant<int, 2>(), one, no);
 }
 
 // Workgroups of the backward pass, each of which leaves one part of the weight's gradient: one a compute unit where it has enough
 // waves of its own and asks ahead, else two.  bf16, us with 256 and 512: 8192x4096 47.8 and 51.8, with dropout (more arithmetic, and
-// no asking ahead) 74.6 and 64.3; 16384x2048 63.0 and 49.0, but 1000x2047 fp32 11.3 and 12.0: too few rows each to make up for the parts.
+// no asking ahead) 74.6 and 64.3; of one team of four waves each 1000x2047 fp32 11.3 and 12.0: too few rows each to make up for the parts.
 constexpr int64_t kMostParts = 512;
 static int64_t backward_groups(int64_t rows, int64_t n, bool drop)
 {
-    const int64_t teams = n <= 1024 ? (rows + 3) / 4 : rows;
-    const bool small = n <= 512 || (n > 1024 && n <= 2048), two = n <= 16384 && (drop || small) && teams >= 4 * kMostParts;
+    const int64_t teams = n <= 1024 || four_teams(rows, n) ? (rows + 3) / 4 : rows;
+    const bool two = (n <= 512 || (drop && n <= 16384 && (n <= 1024 || n > 2048))) && teams >= 4 * kMostParts;
     const int64_t most = two ? kMostParts : kMostParts / 2;
     return teams < 1 ? 1 : teams < most ? teams : most;
 }
@@ -474,7 +499,7 @@ gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t
     return with_types(dtype, weight_dtype, [&](auto t, auto w) {
         typedef decltype(t) T;
         typedef decltype(w) W;
-        return with_team(n, [&](auto wpr, auto steps, auto tiny) {
+        return with_team(rows, n, [&](auto wpr, auto steps, auto tiny) {
             constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value;
             constexpr bool TINY = decltype(tiny)::value;
             const int64_t blocks = (rows + kTeams<WPR> - 1) / kTeams<WPR>;
@@ -516,22 +541,24 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
                 rms_norm_backward_long_kernel<T, W><<<(unsigned)groups, kLongBlock, 32 * (unsigned)p.units, stream>>>(p);
                 return launched();
             }
-            return with_backward_team(n, [&](auto wpr, auto steps, auto tiny) {
-                constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value;
+            return with_backward_team(rows, n, [&](auto wpr, auto steps, auto of, auto tiny) {
+                constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value, TEAMS = decltype(of)::value;
                 constexpr bool TINY = decltype(tiny)::value, kAhead = WPR < 16;      // as far as the registers reach
                 auto with_dsum = [&](auto there) {
                     constexpr bool DSUM = decltype(there)::value;
-                    return groups == kMostParts && drop ? rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, DSUM, false> : rms_norm_backward_kernel<T, W, WPR, STEPS, TINY, DSUM, kAhead>;
+                    constexpr bool kTwo = kAhead && WPR != 4;          // where there may be two workgroups a compute unit, with dropout
+                    return kTwo && groups == kMostParts && drop ? rms_norm_backward_kernel<T, W, WPR, STEPS, TEAMS, TINY, DSUM, !kTwo && kAhead>
+                                                                : rms_norm_backward_kernel<T, W, WPR, STEPS, TEAMS, TINY, DSUM, kAhead>;
                 };
                 auto kernel = dsum ? with_dsum(std::true_type()) : with_dsum(std::false_type());
-                kernel<<<(unsigned)groups, kThreads<WPR>, 0, stream>>>(p);
+                kernel<<<(unsigned)groups, 64 * WPR * TEAMS, 0, stream>>>(p);
                 return launched();
             });
         });
         if (launch != GQ_OK) return launch;
     }
     if (!dweight_out) return GQ_OK;
-    weight_sum_kernel<<<(unsigned)((n + 63) / 64), 256, 0, stream>>>((const float *)workspace, rows > 0 ? (int)groups : 0, (int)n, (int)pitch8(n), dweight_out);
+    weight_sum_kernel<<<(unsigned)((n + kSumColumns - 1) / kSumColumns), 256, 0, stream>>>((const float *)workspace, rows > 0 ? (int)groups : 0, (int)n, (int)pitch8(n), dweight_out);
     return launched();
 }
 

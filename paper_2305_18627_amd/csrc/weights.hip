@@ -44,8 +44,8 @@ __device__ __forceinline__ uint32_t eight_nibbles(const float *q)
 
 // A lane owns UNITS units, each of eight consecutive columns (16 or 32 bytes of weights, one word of codes), a group is 4, 8 or 16
 // neighbouring lanes: the maximum goes round them by DPP within a row of 16 lanes.  Units past the row's last column (a row
-// is padded to whole groups of units) hold zeros; those within the padding of the row's codes write them.  Bound by memory: read
-// once, written once.
+// is padded to whole groups of units) hold zeros; those within the padding of the row's codes write them.  Bound by memory, read
+// once, written once: 8192x8192 bf16, groups of 128, 32.3 us, 5.2 TB/s; 1001x4999 fp32 6.3 us.
 template <typename T, typename S, int GROUP, bool TINY, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per_row, int groups, uint32_t row_words, uint32_t *codes, S *scales)
@@ -87,7 +87,8 @@ group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per
     }
 }
 
-// The same units.
+// value = code scale.  The same units, a word of codes and a scale for 16 or 32 bytes written.  Bound by its writes: 8192x8192 bf16 29.3 us,
+// 5.8 TB/s; 1001x4999 fp32 8.0 us.
 template <typename T, typename S, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, uint32_t units_per_row, int group_shift, int groups,
@@ -118,8 +119,8 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
 
 using namespace gq;
 
-// Units a lane: 4 keep enough in flight in long launches, in short ones more lanes do (quantise 8192x8192 bf16: 47.1, 44.9 and 43.7 us
-// with 1, 2 and 4, unfold 35.1, 33.5, 32.0; 2048x4096: 8.1, 7.9, 9.4 and 5.8, 5.9, 6.7; 128x4096: 3.0, 3.8, 5.6 and 1.9, 2.1, 2.5).
+// Units a lane: 4 keep enough in flight in long launches, in short ones more lanes do (quantise 8192x8192 bf16, with its scale still a division: 47.1, 44.9
+// and 43.7 us with 1, 2 and 4, unfold 35.1, 33.5, 32.0; 2048x4096: 8.1, 7.9, 9.4 and 5.8, 5.9, 6.7; 128x4096: 3.0, 3.8, 5.6 and 1.9, 2.1, 2.5).
 constexpr int64_t kLongWeights = 1 << 21;
 // rows of whole groups: codes and scales of a row end where the next one's begin, the matrix is one row
 static bool is_flat(int64_t rows, int64_t cols, int group) { return cols % group == 0 && flat_fits(rows * (cols / 8)); }
