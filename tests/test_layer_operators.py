@@ -811,3 +811,61 @@ def test_on_another_stream_and_from_a_graph():
         step(eager)
         torch.cuda.synchronize()
         assert same(eager, want) and all(same(got, want) for _, got, _ in graphs)
+
+
+# ---- more than 2^32 elements or bytes: the last rows are those of a call on them alone ------------------------------
+
+def filled(rows, n):
+    return torch.empty(rows, n, dtype=torch.bfloat16, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(rows))
+
+
+@gpu
+@pytest.mark.parametrize("n", [65_536, 65_535])
+def test_dropout_beyond_32_bits(n):
+    rows, last = 66_000, 65_992
+    x = filled(rows, n)
+    out, tail = torch.empty_like(x), torch.empty_like(x[last:])
+    gq.dropout(x, gq.make_dropout(0.3, 9), out)
+    gq.dropout(x[last:], gq.make_dropout(0.3, 9, index_base=65_536 * last), tail)
+    assert torch.equal(out[last:], tail) and 0.29 < float((tail == 0).float().mean()) < 0.31
+
+
+@gpu
+@pytest.mark.parametrize("n", [4096, 4095])
+def test_rms_norm_beyond_32_bits(n):
+    rows, last = 1_050_000, 1_049_992
+    x, w = filled(rows, n), torch.ones(n, device=DEV)
+    out, h = torch.empty_like(x), torch.empty_like(x)
+    rstd, tail, th, tr = torch.empty(rows, device=DEV), torch.empty_like(x[last:]), torch.empty_like(x[last:]), torch.empty(8, device=DEV)
+    drop, part = gq.make_dropout(0.3, 9, rng_bits=16), gq.make_dropout(0.3, 9, index_base=4096 * last, rng_bits=16)
+    gq.rms_norm(x, w, 1e-5, out, sum_out=h, rstd_out=rstd, drop=drop)
+    gq.rms_norm(x[last:], w, 1e-5, tail, sum_out=th, rstd_out=tr, drop=part)
+    assert torch.equal(out[last:], tail) and torch.equal(h[last:], th) and torch.equal(rstd[last:], tr)
+    gq.rms_norm_backward(x, h, w, rstd, out, drop=drop)
+    gq.rms_norm_backward(x[last:], th, w, tr, tail, drop=part)
+    assert torch.equal(out[last:], tail)
+
+
+@gpu
+@pytest.mark.parametrize("cols", [16_384, 16_380])
+def test_weights_beyond_32_bits(cols):
+    rows, last, group = 530_000, 529_992, 64
+    w = filled(rows, cols)
+    codes = torch.empty(rows, gq.w4_row_bytes(cols), dtype=torch.uint8, device=DEV)
+    scales = torch.empty(rows, -(-cols // group), device=DEV)
+    gq.group_quantize(w, group, codes, scales)
+    tc, ts = torch.empty_like(codes[last:]), torch.empty_like(scales[last:])
+    gq.group_quantize(w[last:], group, tc, ts)
+    assert codes.numel() > 1 << 32 and torch.equal(codes[last:], tc) and torch.equal(scales[last:], ts)
+    x = filled(9, cols)
+    for m in (1, 9):
+        y, t = torch.empty(m, rows, device=DEV), torch.empty(m, 8, device=DEV)
+        gq.w4_matvec(x[:m], codes, scales, group, y)
+        gq.w4_matvec(x[:m], tc, ts, group, t)
+        want, tol = plain_matvec(x[:m].cpu(), None, unpacked(tc, cols)[:, :cols], ts, group, None)
+        close(y[:, last:], want, tol)
+        close(t, want, tol)
+    gq.group_dequantize(codes, scales, group, w)
+    t = torch.empty_like(w[last:])
+    gq.group_dequantize(tc, ts, group, t)
+    assert torch.equal(w[last:], t)
