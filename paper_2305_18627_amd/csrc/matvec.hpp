@@ -365,9 +365,10 @@ w4_matvec_kernel(MatvecArgs p)
         // Codes are asked for two steps ahead, x one.  No branch is around a load, for what is loaded on one way only is waited for where the
         // ways join: past the last step its loads come again.  us before and after both: 61 rows of x, 14335x4095, groups of 32, f16 34.3
         // and 29.8; 64 rows, 8192x8192 29.7, 26.9, 28672x8192 75, 68; 64x14000 33.7, 28.3.  Three sets of codes only as far as 128
-        // registers reach (else they spill: 32 rows, 4096x4096, groups of 32 9.0 and 13.4), and not for 16 rows in int8 (12.6, 13.7).
+        // registers reach (else they spill: 32 rows, 4096x4096, groups of 32 9.0 and 13.4): 45 words of codes, scales and x, or 56 where the
+        // groups' products stay apart and a lane's x is little; and not for 16 rows in int8 (12.6, 13.7).
         constexpr int kWords = 3 * (4 * U + kScaleWords) + kAhead * (int)sizeof(Raw) / 4;
-        constexpr int kSets = MT <= 2 && sizeof(X) * MT >= 2 && kWords <= 45 ? 3 : 2;
+        constexpr int kSets = MT <= 2 && sizeof(X) * MT >= 2 && kWords <= (MT == 2 && WK == 2 ? 56 : 45) ? 3 : 2;
         Fetched f[kSets];
         clear();
         if (steps > 0) {
@@ -427,7 +428,8 @@ static gq_status launch_matvec(const MatvecArgs &p, hipStream_t stream)
 //   8192x8192   32: 17.5, 64: 24.4, 16: 24.7       |  slices of 16, 64: 24.2, of 32, 32: 25.2, 64: 29.4 |  slices of 32, 64: 30.0, 32: 45.8
 //   14336x4096  64: 14.2, 32: 15.5                 |  64: 17.0, 32: 19.6                                |  slices of 32, 128: 26.0, of 64, 64: 26.8
 //   28672x8192  64 (8 waves): 38.2, 128: 46.3, 64 (16 waves): 48.5  |  64 (8 waves): 50.1, 128: 51.7    |  128: 72.3, slices of 32, 128: 93.7
-// (taken with codes one step ahead; the first of each now: 6.3, 8.9, 12.3; 16.8, 22.8, 26.9; 13.7, 17.0, 23.7; 39.8, 51.5, 68)
+// (taken with codes one step ahead; the first of each now: 6.3, 8.9, 12.3; 16.8, 22.8, 26.9; 13.7, 17.0, 23.7; 39.8, 50.7, 68.  With them two ahead
+// 32 rows of x take 128 rows a workgroup from 1024 tiles on: 17000x4096 22.6, with 64 24.1, 20000x8192 42.3, 47.2, 28672x8192 46.8, 50.0)
 template <typename X, typename S, int GROUP> static gq_status matvec_of_group(MatvecArgs p, hipStream_t stream)
 {
     const int64_t tiles = (p.rows + 15) / 16;
@@ -448,7 +450,7 @@ template <typename X, typename S, int GROUP> static gq_status matvec_of_group(Ma
     if (p.m <= 32)
         return size == 0   ? launch_matvec<X, S, GROUP, 1, 2, 8, 2, false>(p, stream)
                : size == 1 ? launch_matvec<X, S, GROUP, 2, 2, 8, 1, false>(p, stream)
-               : size == 2 ? launch_matvec<X, S, GROUP, 2, 4, 4, 2, false>(p, stream) : launch_matvec<X, S, GROUP, 2, 4, 2, 2, false>(p, stream);
+               : size == 2 ? launch_matvec<X, S, GROUP, 2, 4, 4, 2, false>(p, stream) : launch_matvec<X, S, GROUP, 2, 8, 2, 2, false>(p, stream);
     return size == 0   ? launch_matvec<X, S, GROUP, 2, 2, 8, 1, false>(p, stream)
            : size == 1 ? launch_matvec<X, S, GROUP, 2, 4, 4, 2, false>(p, stream)
            : size == 2 ? launch_matvec<X, S, GROUP, 2, 8, 2, 2, false>(p, stream) : launch_matvec<X, S, GROUP, 4, 8, 2, 2, false>(p, stream);
