@@ -45,7 +45,8 @@ __device__ __forceinline__ uint32_t eight_nibbles(const float *q)
 // A lane owns UNITS units, each of eight consecutive columns (16 or 32 bytes of weights, one word of codes), a group is 4, 8 or 16
 // neighbouring lanes: the maximum goes round them by DPP within a row of 16 lanes.  Units past the row's last column (a row
 // is padded to whole groups of units) hold zeros; those within the padding of the row's codes write them.  Bound by memory, read
-// once, written once: 8192x8192 bf16, groups of 128, 32.3 us, 5.2 TB/s; 1001x4999 fp32 6.3 us.
+// once, written once: 8192x8192 bf16, groups of 128, 32.3 us with unfolding in between, 5.2 TB/s, and
+// 38.7 in a loop of its own; fp32, groups of 32, 56.5; 1001x4999 fp32 6.4.
 template <typename T, typename S, int GROUP, bool TINY, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per_row, int groups, uint32_t row_words, uint32_t *codes, S *scales)
@@ -87,13 +88,15 @@ group_quantize_kernel(const T *w, int64_t rows, int64_t cols, uint32_t units_per
     }
 }
 
-// value = code scale.  The same units, a word of codes and a scale for 16 or 32 bytes written.  Bound by its writes: 8192x8192 bf16 29.3 us,
-// 5.8 TB/s; 1001x4999 fp32 8.0 us.
+// value = code scale.  A lane owns UNITS units of 16 bytes of values, eight columns and a word of codes, or four (binary32) and half a word, so
+// that a wave's stores lie next to each other.  Bound by its writes: 8192x8192 bf16 29.3 us, 5.8 TB/s,
+// fp32 57 us, 5.3 TB/s (with eight columns a lane 76); 8001x4999 fp32 45.5 (53.8), 1001x4999 7.8 (7.7).
 template <typename T, typename S, bool FLAT, int UNITS>
 __global__ void __launch_bounds__(kBlock)
 group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, int64_t cols, uint32_t units_per_row, int group_shift, int groups,
                         uint32_t row_words, T *out)
 {
+    constexpr int kPer = 16 / sizeof(T), kShift = kPer == 8 ? 3 : 2;
     RowUnit at[UNITS];
     uint32_t word[UNITS];
     S scale[UNITS];
@@ -102,16 +105,30 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
         at[k] = row_unit<UNITS, FLAT>(blockIdx.x, k, units_per_row);
         const int64_t row = FLAT ? 0 : at[k].row < rows ? at[k].row : rows - 1;
         const uint32_t unit = FLAT ? min(at[k].unit, units_per_row - 1) : at[k].unit;
-        word[k] = __builtin_nontemporal_load(codes + row * row_words + unit);
-        scale[k] = scales[row * groups + (unit >> (group_shift - 3))];
+        word[k] = __builtin_nontemporal_load(codes + row * row_words + (unit >> (3 - kShift)));
+        scale[k] = scales[row * groups + (unit >> (group_shift - kShift))];
     }
 #pragma unroll
     for (int k = 0; k < UNITS; k++) {
         if (at[k].row >= rows) return;
+        const uint32_t w = kPer == 8 ? word[k] : word[k] >> 16 * (at[k].unit & 1);
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = (float)((int)(word[k] << (28 - 4 * i)) >> 28) * (float)scale[k];
-        store8(out + (FLAT ? 0 : at[k].row) * cols + (int64_t)at[k].unit * 8, cols - (int64_t)at[k].unit * 8, v);
+        for (int i = 0; i < kPer; i++) v[i] = (float)((int)(w << (28 - 4 * i)) >> 28) * (float)scale[k];
+        T *to = out + (FLAT ? 0 : at[k].row) * cols + (int64_t)at[k].unit * kPer;
+        const int64_t left = cols - (int64_t)at[k].unit * kPer;
+        if constexpr (kPer == 8) {
+            store8(to, left, v);
+        } else if (left >= 4) {
+            typename Chunk<4>::type c;
+#pragma unroll
+            for (int i = 0; i < 4; i++) c[i] = __float_as_uint(v[i]);
+            *reinterpret_cast<typename Chunk<4>::type *>(to) = c;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (i < left) to[i] = v[i];
+        }
     }
 }
 
@@ -123,7 +140,7 @@ using namespace gq;
 // and 43.7 us with 1, 2 and 4, unfold 35.1, 33.5, 32.0; 2048x4096: 8.1, 7.9, 9.4 and 5.8, 5.9, 6.7; 128x4096: 3.0, 3.8, 5.6 and 1.9, 2.1, 2.5).
 constexpr int64_t kLongWeights = 1 << 21;
 // rows of whole groups: codes and scales of a row end where the next one's begin, the matrix is one row
-static bool is_flat(int64_t rows, int64_t cols, int group) { return cols % group == 0 && flat_fits(rows * (cols / 8)); }
+static bool is_flat(int64_t rows, int64_t cols, int group) { return cols % group == 0 && flat_fits(rows * (cols / 4)); }
 static bool long_launch(int64_t units, int64_t cols) { return cols >= 8 && units >= kLongWeights; }
 
 extern "C" {
@@ -174,7 +191,7 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
     if (!aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, 16)) return GQ_ERR_INVALID_ARG;
     const bool flat = is_flat(rows, cols, group);
     if (flat) cols *= rows, rows = 1;
-    const int64_t row_words = (cols + 31) / 32 * 4, per_row = (cols + 7) / 8, units = rows * per_row;
+    const int64_t row_words = (cols + 31) / 32 * 4, per = 16 / (int64_t)dtype_size(dtype), per_row = (cols + per - 1) / per, units = rows * per_row;
     const int64_t per_block = (long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
