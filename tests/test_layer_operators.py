@@ -387,6 +387,32 @@ def test_rms_norm_in_8_bits(n, name, weight, kind):
 
 
 @gpu
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("n", [2049, 2500, 4096, 5003, 6144, 6200, 8192])
+def test_rms_norm_of_many_rows(n, name):
+    """Above 256 rows other teams of waves take rows of these lengths."""
+    rows, t = 259, TYPES[name]
+    x, res, w = norm_inputs(rows, n, t, t, seed=6)
+    drop = gq.make_dropout(0.25, SEED, 2, 8, 32)
+    h, dh, rstd, rel, y, dy = plain_norm(x, res, w, 1e-5, drop)
+    s, out, rs, codes = Guarded((rows, n), t), Guarded((rows, n), t), Guarded((rows,), torch.float32), Guarded((rows, n), torch.int8)
+    xd, rd, wd = x.to(DEV), res.to(DEV), w.to(DEV)
+    sc = torch.empty(rows, device=DEV)
+    gq.rms_norm(xd, wd, 1e-5, codes.t, residual=rd, scales_out=sc, drop=drop)
+    gq.rms_norm(xd, wd, 1e-5, out.t, residual=rd, sum_out=s.t, rstd_out=rs.t, drop=drop)
+    close(s.t, h, dh + half_step(t) * (h.abs() + dh) + least(t))
+    close(rs.t, rstd[:, 0], (rstd * rel)[:, 0])
+    close(out.t, y, dy + half_step(t) * (y.abs() + dy) + least(t))
+    want = y.abs().amax(1) / 127.0
+    close(sc, want, dy.amax(1) / 127.0 + 2 * U * want)
+    scale = sc.double().cpu()[:, None]
+    close(codes.t, (y / scale).clamp(-127, 127), dy / scale + 3 * U * (y / scale).abs() + 0.5)
+    assert s.intact() and out.intact() and rs.intact() and codes.intact()
+    gq.rms_norm(xd, wd, 1e-5, xd, residual=rd, sum_out=rd, drop=drop)
+    assert torch.equal(xd, out.t) and torch.equal(rd, s.t)
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["i8", "e4m3"])
 def test_rms_norm_rows_that_are_not_finite_or_hardly_anything(kind):
     ot, n = (torch.int8 if kind == "i8" else torch.float8_e4m3fn), 300
@@ -668,7 +694,8 @@ def test_w4_matvec_rows_are_apart(x_type):
 @pytest.mark.parametrize("x_type,out,scale,group", [("bf16", "f32", "bf16", 128), ("f16", "f16", "f32", 64), ("i8", "f32", "bf16", 32)])
 @pytest.mark.parametrize("m,rows,cols", [(1, 9001, 260), (2, 12000, 2100), (3, 9001, 260), (8, 17001, 136), (8, 40, 9001), (12, 5000, 1100), (12, 9001, 260),
                                          (12, 12000, 136), (12, 17001, 136), (30, 5000, 600), (30, 9001, 260), (30, 12000, 136), (30, 17001, 136),
-                                         (50, 5000, 600), (50, 9001, 260), (50, 12000, 136), (50, 17001, 136), (100, 9001, 136)])
+                                         (50, 5000, 600), (50, 9001, 260), (50, 12000, 136), (50, 17001, 136), (100, 9001, 136),
+                                         (40, 700, 4200), (12, 12000, 3200), (50, 12000, 1700), (30, 17001, 1700)])       # several steps
 def test_w4_matvec_of_many_rows(m, rows, cols, group, x_type, out, scale):
     g = torch.Generator().manual_seed(m * 7919 + rows * 31 + cols + group)
     q, codes, scales = weights(g, rows, cols, group, TYPES[scale])
