@@ -288,7 +288,8 @@ w4_matvec_kernel(MatvecArgs p)
             float v = 0.0f;
 #pragma unroll
             for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
-            if (p.x_scales) v *= A::kUnit * p.x_scales[mm];
+            // the 16 of int8 sums is taken out of the sum: a scale of the row may be subnormal, and its product with 1 / 16 is then rounded
+            if (p.x_scales) v = v * A::kUnit * p.x_scales[mm];
             const int64_t at = (int64_t)mm * p.rows + row;
             if (p.y_dtype == GQ_F32) ((float *)p.y)[at] = p.bias ? v + ((const float *)p.bias)[row] : v;
             else if (p.y_dtype == GQ_BF16) ((bf16 *)p.y)[at] = (bf16)(p.bias ? v + (float)((const bf16 *)p.bias)[row] : v);

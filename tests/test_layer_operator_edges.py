@@ -1,0 +1,52 @@
+"""The layers around the gradient exchange where numbers, sizes and callers go to their ends: scales near the ends of binary32, long sums of
+weights' gradients, every shape of workgroup over several steps, second rows and second tiles, long launches of every type."""
+import math
+
+import pytest
+import torch
+
+import paper_2305_18627_amd as gq
+import test_layer_operators as L
+
+gpu = pytest.mark.gpu
+DEV, U, TYPES, close = L.DEV, L.U, L.TYPES, L.close
+
+
+def device_weights(g, rows, cols, group, st):
+    """Random codes and scales made on the GPU: (codes as numbers, packed, scales)."""
+    q = torch.zeros(rows, 2 * gq.w4_row_bytes(cols), dtype=torch.int16, device=DEV)
+    q[:, :cols] = torch.randint(-8, 8, (rows, cols), generator=g, device=DEV, dtype=torch.int16)
+    codes = ((q[:, 0::2] & 15) | ((q[:, 1::2] & 15) << 4)).to(torch.uint8)
+    scales = (0.01 + torch.rand(rows, -(-cols // group), generator=g, device=DEV)).to(st)
+    return q[:, :cols], codes, scales
+
+
+def exact_matvec(x, xs, q, scales, group):
+    """(y in 64 bits, its tolerance before the output's rounding), a group of columns at a time: the roundings that plain_matvec counts."""
+    y, off = (torch.zeros(x.shape[0], q.shape[0], dtype=torch.float64, device=DEV) for _ in range(2))
+    for k in range(scales.shape[1]):
+        at, s = slice(k * group, min((k + 1) * group, q.shape[1])), scales[:, k].double()
+        xg = x[:, at].double()
+        part = (xg @ q[:, at].double().t().contiguous()) * s
+        y += part
+        off += (scales.shape[1] + 3) * U * part.abs()
+        if xs is None:
+            off += (group + 4) * U * 32 * xg.abs().sum(1, keepdim=True) * s.abs()
+    return (y, off) if xs is None else (y * xs.double()[:, None], off * xs.double()[:, None].abs())
+
+
+# ---- the product near the ends of binary32 --------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m", [1, 3, 12, 40, 100])
+def test_int8_product_under_subnormal_scales_of_rows(m, group):
+    """Scales of rows that a norm of tiny rows writes: subnormal, so that a product with a power of two would round them."""
+    g = torch.Generator(DEV).manual_seed(m)
+    q, codes, scales = device_weights(g, 200, 300, group, torch.float32)
+    scales *= 2.0 ** 30
+    x = torch.randint(-127, 128, (m, 300), generator=g, device=DEV).to(torch.int8)
+    xs = ((16 * torch.arange(1000, 1000 + m, dtype=torch.float64) + 8) * 2.0 ** -149).float().to(DEV)
+    y = torch.empty(m, 200, device=DEV)
+    gq.w4_matvec(x, codes, scales, group, y, x_scales=xs)
+    close(y, *exact_matvec(x, xs, q, scales, group))
