@@ -416,8 +416,8 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
  *   y         device [m][rows] of y_dtype: GQ_F32, GQ_BF16 or GQ_F16
  * Products of int8 activations are summed exactly within a group.  Sums of GQ_BF16 and GQ_F16 activations are formed with the
  * codes moved by 24 (matrix instructions take 24 + code) and corrected by 24 times the sum of x: in binary32, so exact to a few
- * 2^-24 of 24 sum |x| over up to 128 columns.  A row of x that holds an infinity or a NaN gives NaN, and so may finite ones of
- * which 31 times a group's sum of |x| leaves binary32. */
+ * 2^-24 of 24 sum |x| over up to 128 columns; where that leaves binary32 the sum is formed again in binary64.  A row of x that
+ * holds an infinity or a NaN gives NaN, whatever the codes. */
 gq_status gq_w4_matvec(const void *x, const float *x_scales, int64_t m, gq_dtype x_dtype, const void *codes, const void *scales,
                        gq_dtype scale_dtype, int64_t rows, int64_t cols, int group, const void *bias, void *y, gq_dtype y_dtype,
                        void *hip_stream);

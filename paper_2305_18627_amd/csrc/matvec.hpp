@@ -279,6 +279,22 @@ w4_matvec_kernel(MatvecArgs p)
 #pragma unroll
         for (int i = 0; i < MT; i++) *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + (i * 64 + lane) * 4) = acc[i];
     };
+    // A product whose sum is not finite, once more in binary64: the sums of 24 |x| of a bfloat16 row may leave binary32 where its product does
+    // not.  One lane a product, a column at a time, in few registers: slow, and rare.  The first infinity or NaN ends it, as does a scale of NaN.
+    auto sum_again = [&](int row_of_x, int row) {
+        const Bits *at = (const Bits *)x + (int64_t)row_of_x * p.cols;
+        const uint8_t *codes = p.codes + (int64_t)row * p.row_bytes;
+        const S *scales = (const S *)p.scales + (int64_t)row * p.groups;
+        double s = 0.0;
+#pragma unroll 1
+        for (int c = 0; c < p.cols && s == s; c++) {
+            const float f = __uint_as_float((uint32_t)at[c] << 16);
+            if (!(__builtin_fabsf(f) <= 3.402823466e+38f)) return __builtin_nanf("");
+            const int code = (int)((uint32_t)codes[c / 2] << (28 - 4 * (c & 1))) >> 28;
+            s += (double)f * ((double)(float)scales[c / GROUP] * (double)code);
+        }
+        return (float)s;
+    };
     auto join = [&](const float *part, int tile_of_rows) {
         for (int e = threadIdx.x; e < WN * kPerWave; e += kThreads) {
             // e: (wave of rows, tile, m within it, row within it), the row fastest
@@ -288,6 +304,8 @@ w4_matvec_kernel(MatvecArgs p)
             float v = 0.0f;
 #pragma unroll
             for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
+            if constexpr (std::is_same<X, bf16>::value)
+                if (!(__builtin_fabsf(v) <= 3.402823466e+38f)) v = sum_again(mm - first_m, row);
             // the 16 of int8 sums is taken out of the sum: a scale of the row may be subnormal, and its product with 1 / 16 is then rounded
             if (p.x_scales) v = v * A::kUnit * p.x_scales[mm];
             const int64_t at = (int64_t)mm * p.rows + row;

@@ -50,3 +50,36 @@ def test_int8_product_under_subnormal_scales_of_rows(m, group):
     y = torch.empty(m, 200, device=DEV)
     gq.w4_matvec(x, codes, scales, group, y, x_scales=xs)
     close(y, *exact_matvec(x, xs, q, scales, group))
+
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m", [1, 5, 12, 40, 100])
+def test_products_of_large_finite_rows_are_numbers(m, group):
+    """bfloat16 rows whose sums of 24 |x| are beyond binary32, though their products are not; rows beside them keep their bits."""
+    g = torch.Generator(DEV).manual_seed(m + group)
+    rows, cols = 150, 300
+    q, codes, scales = device_weights(g, rows, cols, group, torch.float32)
+    scales *= 2.0 ** -20
+    x = torch.randn(m, cols, generator=g, device=DEV).to(torch.bfloat16)
+    clean = torch.empty(m, rows, device=DEV)
+    gq.w4_matvec(x, codes, scales, group, clean)
+    large = torch.arange(m, device=DEV) % 3 == 0
+    x[large] = (x[large].float() * 2.0 ** 125).to(torch.bfloat16)
+    assert torch.isfinite(x).all()
+    y = torch.empty(m, rows, device=DEV)
+    gq.w4_matvec(x, codes, scales, group, y)
+    want, tol = exact_matvec(x, None, q, scales, group)
+    assert float(want.abs().max()) < 2.0 ** 126
+    close(y, want, tol)
+    assert torch.equal(y[~large], clean[~large])
+    # where the product itself is beyond binary32 it is an infinity of its sign
+    scales *= 2.0 ** 30
+    gq.w4_matvec(x, codes, scales, group, y)
+    want, tol = want * 2.0 ** 30, tol * 2.0 ** 30
+    top = float(torch.finfo(torch.float32).max)
+    sure = (want.abs() + tol < top) | (want.abs() - tol > 2.0 * top)
+    beyond = want.abs() > top
+    want[beyond] *= float("inf")
+    assert bool(sure[large].any()) and bool(beyond[sure].any())
+    close(y[sure], want[sure], tol[sure])
