@@ -78,6 +78,8 @@ template <> struct Act<int8_t> {
     }
 };
 
+__device__ __forceinline__ bool is_finite(float f) { return __builtin_fabsf(f) <= 3.402823466e+38f; }
+
 // d[j] of lane group q (lanes 16 q .. 16 q + 15) becomes d[q] of lane group j
 __device__ __forceinline__ void transpose4(uint32_t *d)
 {
@@ -279,35 +281,45 @@ w4_matvec_kernel(MatvecArgs p)
 #pragma unroll
         for (int i = 0; i < MT; i++) *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + (i * 64 + lane) * 4) = acc[i];
     };
-    // A product whose sum is not finite, once more in binary64: the sums of 24 |x| of a bfloat16 row may leave binary32 where its product does
-    // not.  One lane a product, a column at a time, in few registers: slow, and rare.  The first infinity or NaN ends it, as does a scale of NaN.
-    auto sum_again = [&](int row_of_x, int row) {
-        const Bits *at = (const Bits *)x + (int64_t)row_of_x * p.cols;
-        const uint8_t *codes = p.codes + (int64_t)row * p.row_bytes;
-        const S *scales = (const S *)p.scales + (int64_t)row * p.groups;
-        double s = 0.0;
+    // Products whose sums are not finite, once more in binary64: the sums of 24 |x| of a bfloat16 row, and 16 times the sum of int8 codes, may
+    // leave binary32 where the product does not.  One after another, the whole wave at each; a row of x that is not finite ends at once, for
+    // all its products.  A column a lane, in few registers, for it is rare: 64 rows of x, 28672x8192, groups of 64, take 20 ms where all
+    // products go this way, 1.3 where each row of x ends in an infinity, 0.08 otherwise.
+    auto once_more = [&](bool wanted, int row_of_x, int row, float &v) {
+        for (uint64_t left = __ballot(wanted && !is_finite(v)); left != 0;) {
+            const int l = __builtin_ctzll(left), rx = __builtin_amdgcn_readlane(row_of_x, l), rw = __builtin_amdgcn_readlane(row, l);
+            const X *at = x + (int64_t)rx * p.cols;
+            const uint8_t *codes = p.codes + rw * p.row_bytes;
+            const S *scales = (const S *)p.scales + (int64_t)rw * p.groups;
+            double s = 0.0;
+            bool finite = true;
 #pragma unroll 1
-        for (int c = 0; c < p.cols && s == s; c++) {
-            const float f = __uint_as_float((uint32_t)at[c] << 16);
-            if (!(__builtin_fabsf(f) <= 3.402823466e+38f)) return __builtin_nanf("");
-            const int code = (int)((uint32_t)codes[c / 2] << (28 - 4 * (c & 1))) >> 28;
-            s += (double)f * ((double)(float)scales[c / GROUP] * (double)code);
+            for (int first = 0; first < p.cols && __all(finite); first += 64) {
+                const uint32_t c = (uint32_t)min(first + lane, p.cols - 1);
+                const float f = first + lane < p.cols ? (float)at[c] : 0.0f;
+                finite = is_finite(f);
+                s += (double)f * ((double)(float)scales[c / GROUP] * (double)((int)((uint32_t)codes[c / 2] << (28 - 4 * (c & 1))) >> 28));
+            }
+            const bool nan = !__all(finite);
+            s = wave_sum(s);
+            if (nan ? row_of_x == rx : lane == l) v = nan ? __builtin_nanf("") : (float)s;
+            left &= nan ? ~__ballot(row_of_x == rx) : left - 1;
         }
-        return (float)s;
     };
     auto join = [&](const float *part, int tile_of_rows) {
         for (int e = threadIdx.x; e < WN * kPerWave; e += kThreads) {
             // e: (wave of rows, tile, m within it, row within it), the row fastest
             const int w = e / kPerWave, tile = e % kPerWave / 256, mi = e % 256 / 16, ri = e % 16;
             const int mm = first_m + tile * 16 + mi, row = (tile_of_rows * WN + w) * 16 + ri;
-            if (mm >= p.m || row >= p.rows) continue;
+            const bool there = mm < p.m && row < p.rows;
             float v = 0.0f;
 #pragma unroll
             for (int k = 0; k < WK; k++) v += part[(k * WN + w) * kPerWave + (tile * 64 + mi / 4 * 16 + ri) * 4 + mi % 4];
-            if constexpr (std::is_same<X, bf16>::value)
-                if (!(__builtin_fabsf(v) <= 3.402823466e+38f)) v = sum_again(mm - first_m, row);
-            // the 16 of int8 sums is taken out of the sum: a scale of the row may be subnormal, and its product with 1 / 16 is then rounded
-            if (p.x_scales) v = v * A::kUnit * p.x_scales[mm];
+            if (!A::kMoved) v *= A::kUnit;
+            if constexpr (!std::is_same<X, f16>::value) once_more(there, mm - first_m, row, v);      // binary16 is too small for either
+            if (!there) continue;
+            // the 16 of int8 sums has been taken out of the sum: the row's scale may be subnormal, and its product with 1 / 16 is then rounded
+            if (p.x_scales) v *= p.x_scales[mm];
             const int64_t at = (int64_t)mm * p.rows + row;
             if (p.y_dtype == GQ_F32) ((float *)p.y)[at] = p.bias ? v + ((const float *)p.bias)[row] : v;
             else if (p.y_dtype == GQ_BF16) ((bf16 *)p.y)[at] = (bf16)(p.bias ? v + (float)((const bf16 *)p.bias)[row] : v);

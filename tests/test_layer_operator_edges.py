@@ -53,6 +53,21 @@ def test_int8_product_under_subnormal_scales_of_rows(m, group):
 
 
 @gpu
+@pytest.mark.parametrize("m", [1, 3, 12, 40, 100])
+@pytest.mark.parametrize("cols", [32, 64])
+def test_int8_product_of_sums_near_the_end_of_binary32(cols, m):
+    """Scales of weights under which the sum is below 2^126, and scales of rows that bring it back."""
+    codes = torch.full((70, gq.w4_row_bytes(cols)), 0x77, dtype=torch.uint8, device=DEV)
+    scales = torch.full((70, 1), 2.0 ** 110, device=DEV)
+    x = torch.full((m, cols), 127, dtype=torch.int8, device=DEV)
+    xs = torch.full((m,), 2.0 ** -10, device=DEV)
+    y = torch.empty(m, 70, device=DEV)
+    gq.w4_matvec(x, codes, scales, 64, y, x_scales=xs)
+    want = torch.full((m, 70), 7.0 * 127 * cols * 2.0 ** 100, dtype=torch.float64)
+    close(y, want, 2 * U * want)
+
+
+@gpu
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("m", [1, 5, 12, 40, 100])
 def test_products_of_large_finite_rows_are_numbers(m, group):
