@@ -201,9 +201,10 @@ template <typename F> static inline gq_status with_float_type(int t, F &&f)
 }
 
 // 4-bit weights
+constexpr int64_t kMaxWeightCols = 1 << 24;
 static inline gq_status check_weights(int64_t rows, int64_t cols, int group, int scale_dtype)
 {
-    if (!matrix_fits(rows, cols) || rows > (1 << 30) || cols > (1 << 24) || (group != 32 && group != 64 && group != 128)) return GQ_ERR_INVALID_ARG;
+    if (!matrix_fits(rows, cols) || rows > (1 << 30) || cols > kMaxWeightCols || (group != 32 && group != 64 && group != 128)) return GQ_ERR_INVALID_ARG;
     return scale_dtype == GQ_F32 || scale_dtype == GQ_BF16 ? GQ_OK : GQ_ERR_INVALID_ARG;
 }
 template <typename F> static inline gq_status with_scale_type(int t, F &&f) { return t == GQ_F32 ? f(float()) : f(bf16()); }

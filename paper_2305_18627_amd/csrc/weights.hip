@@ -145,7 +145,7 @@ static bool long_launch(int64_t units, int64_t cols) { return cols >= 8 && units
 
 extern "C" {
 
-int64_t gq_w4_row_bytes(int64_t cols) { return cols < 0 || !matrix_fits(1, cols) ? 0 : (cols + 31) / 32 * 16; }
+int64_t gq_w4_row_bytes(int64_t cols) { return cols < 0 || cols > kMaxWeightCols ? 0 : (cols + 31) / 32 * 16; }
 
 gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype dtype, int group, void *codes_out, void *scales_out,
                             gq_dtype scale_dtype, void *hip_stream)

@@ -67,6 +67,10 @@ def test_int8_product_of_sums_near_the_end_of_binary32(cols, m):
     close(y, want, 2 * U * want)
 
 
+def test_row_bytes_of_more_columns_than_the_calls_take():
+    assert gq.w4_row_bytes(1 << 24) == 1 << 23 and gq.w4_row_bytes((1 << 24) + 1) == 0 and gq.w4_row_bytes(1 << 40) == 0
+
+
 @gpu
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("m", [1, 5, 12, 40, 100])
