@@ -290,7 +290,8 @@ def rms_norm_workspace_bytes(rows, n):
 def rms_norm_backward(dy, h, weight, rstd, dx_out, dsum=None, dres_out=None, dweight_out=None, drop=None, workspace=None, stream=None):
     """gq_rms_norm_backward: the gradients of x, of the residual (dres_out, with drop only; else it is dx_out) and of the weight.
     Returns the workspace used (None without dweight_out)."""
-    if workspace is None and dweight_out is not None:
+    # what is no matrix is refused below, as in the other calls
+    if workspace is None and dweight_out is not None and isinstance(dy, torch.Tensor) and dy.dim():
         n = dy.size(-1)
         nbytes = max(rms_norm_workspace_bytes(dy.numel() // n if n else 0, n), 16)
         if stream is None:

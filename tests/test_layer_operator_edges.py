@@ -102,3 +102,13 @@ def test_products_of_large_finite_rows_are_numbers(m, group):
     want[beyond] *= float("inf")
     assert bool(sure[large].any()) and bool(beyond[sure].any())
     close(y[sure], want[sure], tol[sure])
+
+
+# ---- callers ----------------------------------------------------------------------------------------------------------
+
+def test_backward_refuses_what_is_no_matrix_like_the_other_calls():
+    x, w = torch.zeros(2, 8), torch.zeros(8)
+    with pytest.raises(TypeError):
+        gq.rms_norm_backward(None, x, w, w, x, dweight_out=w)
+    with pytest.raises(ValueError):
+        gq.rms_norm_backward(torch.zeros(()), x, w, w, x, dweight_out=w)
