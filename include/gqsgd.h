@@ -380,7 +380,8 @@ gq_status gq_rms_norm(const void *x, const void *residual, int64_t rows, int64_t
  *   drop          the forward call's, or NULL
  *   dres_out      device [rows][n]: dh, the residual's gradient; only with drop (else GQ_ERR_INVALID_ARG), or NULL; may be dsum
  *   dx_out        device [rows][n]: x's gradient: dh, with drop after dropout; may be dy or dsum, not dres_out
- *   dweight_out   device fp32[n], overwritten, or NULL.  Its bits do not depend on scheduling (no atomics).
+ *   dweight_out   device fp32[n], overwritten, or NULL.  Summed in binary64 in at most 512 parts, each of which is rounded to
+ *                 binary32, as is their sum.  Its bits do not depend on scheduling (no atomics).
  *   workspace     device scratch of at least gq_rms_norm_workspace_bytes(rows, n) bytes, 16-byte aligned, where dweight_out is
  *                 given; overwritten; not to be shared by calls that may run concurrently */
 size_t gq_rms_norm_workspace_bytes(int64_t rows, int64_t n);

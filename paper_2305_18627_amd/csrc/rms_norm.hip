@@ -202,10 +202,17 @@ template <typename T> __device__ __forceinline__ void forget(Eight<T> &t)
     }
 }
 
+__device__ __forceinline__ void store_part(float *part, const double *dw)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) *reinterpret_cast<f32x4 *>(part + i) = f32x4{(float)dw[i], (float)dw[i + 1], (float)dw[i + 2], (float)dw[i + 3]};
+}
+
 // dh = dsum + rstd (g - xh mean(g xh)) and dweight = sum over rows of dy xh, with xh = h rstd, g = dy weight: one pass over the rows.
 // A workgroup takes rows (its teams one each) in turn, gridDim.x * teams apart, and keeps the weight's gradient of its columns in
 // registers; its sums go to `parts` and a second kernel adds those up.  AHEAD: the next row is asked for before the current one is
-// reduced, where the registers reach.  dweight stays in binary32: a lane adds up no more than its workgroup's share of the rows.
+// reduced, where the registers reach.  dweight is summed in binary64, where the products are exact, and rounded once a part and once at the
+// end, so that its error does not grow with the rows; sums in binary32 are no faster (8192x4096 bf16 40.5 us with both).
 // Bound by memory: 8192x4096 bf16 with dsum and dropout 61 us, 5.5 TB/s, and 4.8 us for the parts' sum; 1000x2047 fp32, four rows a
 // workgroup one after another, 8.4 and 2.5 us.
 template <typename T, typename W, int WPR, int STEPS, int TEAMS, bool TINY, bool DSUM, bool AHEAD>
@@ -215,7 +222,7 @@ rms_norm_backward_kernel(BackwardArgs p)
     constexpr int kLanes = 64 * WPR, kTeam = TEAMS;
     constexpr bool kTogether = TEAMS > 1 && WPR > 1;                  // there is a barrier in each turn, and several teams at it
     __shared__ double sums[2][kTeam][WPR];
-    __shared__ float joined[kTeam > 1 ? kTeam - 1 : 1][kTeam > 1 ? STEPS * 8 * kLanes : 1];
+    __shared__ double joined[kTeam > 1 ? kTeam - 1 : 1][kTeam > 1 ? STEPS * 8 * kLanes : 1];
     const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
     const int64_t stride = (int64_t)gridDim.x * kTeam;
     struct Row { Eight<T> dy[STEPS], h[STEPS], ds[DSUM ? STEPS : 1]; float rstd; };
@@ -231,13 +238,13 @@ rms_norm_backward_kernel(BackwardArgs p)
     };
     Eight<W> w[STEPS];
     Row now, next;
-    float dw[STEPS][8];
+    double dw[STEPS][8];
 #pragma unroll
     for (int k = 0; k < STEPS; k++) {
         ask8<false, TINY>((const W *)p.weight, p.n, 8 * (lane + k * kLanes), w[k]);
         settle8<TINY>(p.n, 8 * (lane + k * kLanes), w[k]);
 #pragma unroll
-        for (int i = 0; i < 8; i++) dw[k][i] = 0.0f;
+        for (int i = 0; i < 8; i++) dw[k][i] = 0.0;
     }
     int64_t row = (int64_t)blockIdx.x * kTeam + team;
     if (AHEAD && row < p.rows) fetch(row, now);
@@ -257,7 +264,7 @@ rms_norm_backward_kernel(BackwardArgs p)
             for (int i = 0; i < 8; i++) {
                 const float dy = now.dy[k].f(i), xh = now.h[k].f(i) * rstd;
                 s = __builtin_fma((double)(dy * w[k].f(i)), (double)xh, s);
-                dw[k][i] += dy * xh;
+                dw[k][i] = __builtin_fma((double)dy, (double)xh, dw[k][i]);
             }
             __builtin_amdgcn_sched_barrier(0);                        // a unit after another: all at once hold too many registers
         }
@@ -306,78 +313,133 @@ rms_norm_backward_kernel(BackwardArgs p)
     for (int k = 0; k < STEPS; k++) {
         const int u = lane + k * kLanes;
         if (u < p.units) {
-            *reinterpret_cast<f32x4 *>(part + 8 * u) = f32x4{dw[k][0], dw[k][1], dw[k][2], dw[k][3]};
-            *reinterpret_cast<f32x4 *>(part + 8 * u + 4) = f32x4{dw[k][4], dw[k][5], dw[k][6], dw[k][7]};
+            store_part(part + 8 * u, dw[k]);
         }
     }
 }
 
-// The same for rows that the registers of a team do not hold: each is read twice, the weight's gradient is kept in LDS.  The second
-// reading and the round through LDS bound it: 1024x32768 bf16 with dsum 75 us, 3.6 TB/s of the bytes that one reading moves.
+// The same for rows that the registers of a team do not hold beside the weight's gradient: dy and h stay in LDS from the first look at a row to
+// the second, 128 KB for STEPS units a lane; dy alone where that is not enough (binary32 above 16384 columns: h is read again).
+// Bound by memory and what a step does not overlap: with dsum 1024x32768 bf16 66.6 us, 4.0 TB/s (75.8 with each row read twice), fp32 135, 4.0;
+// 4096x16384 bf16 102, 5.3, without dsum 85, 4.7.
 constexpr int kLongBlock = 1024;
-template <typename T, typename W>
+constexpr int kLongLds = 128 * 1024;
+template <typename T, typename W, int STEPS>
 __global__ void __launch_bounds__(kLongBlock)
 rms_norm_backward_long_kernel(BackwardArgs p)
 {
-    constexpr int kWaves = kLongBlock / 64;
-    extern __shared__ f32x4 dw[];                                     // [units][2], each touched by one lane only
+    constexpr int kWaves = kLongBlock / 64, kChunks = sizeof(T) / 2;           // of 16 bytes a unit
+    constexpr bool kKeepH = 2 * STEPS * kChunks * 16 * kLongBlock <= kLongLds;
+    constexpr int kPer = kKeepH ? 2 * kChunks : kChunks;
+    static_assert(STEPS * kPer * 16 * kLongBlock <= kLongLds, "LDS");
+    extern __shared__ u32x4 kept[];                                            // [STEPS][kPer][lanes], each touched by one lane only
     __shared__ double sums[2][kWaves];
-    for (int u = threadIdx.x; u < p.units; u += kLongBlock) dw[2 * u] = dw[2 * u + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    int turn = 0;
+    const int first = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63);       // the wave's first unit
+    auto keep = [&](int at, const Eight<T> &t) {
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) kept[(at + i) * kLongBlock + threadIdx.x] = u32x4{t.w[4 * i], t.w[4 * i + 1], t.w[4 * i + 2], t.w[4 * i + 3]};
+    };
+    auto recall = [&](int at, Eight<T> &t) {
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) {
+            const u32x4 v = kept[(at + i) * kLongBlock + threadIdx.x];
+#pragma unroll
+            for (int j = 0; j < 4; j++) t.w[4 * i + j] = v[j];
+        }
+    };
+    // as far as the registers reach: the next row's units asked for when the current one's are in LDS, and the weight held
+    constexpr bool kAhead = STEPS == 2, kHoldW = STEPS == 2 && sizeof(T) == 2;
+    constexpr int kHeld = kAhead ? STEPS : 1;
+    Eight<T> a[kHeld], b[kHeld];
+    Eight<W> w[kHoldW ? STEPS : 1];
+    double dw[STEPS][8];
+    int turn = 0, t = threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        if (kHoldW) {
+            ask8<false, false>((const W *)p.weight, p.n, 8 * (t + k * kLongBlock), w[kHoldW ? k : 0]);
+            settle8<false>(p.n, 8 * (t + k * kLongBlock), w[kHoldW ? k : 0]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) dw[k][i] = 0.0;
+    }
+    auto ask_row = [&](int64_t row) {
+#pragma unroll
+        for (int k = 0; k < kHeld; k++) {
+            ask8<true, false>((const T *)p.dy + row * p.n, p.n, 8 * (t + k * kLongBlock), a[k]);
+            ask8<kKeepH, false>((const T *)p.h + row * p.n, p.n, 8 * (t + k * kLongBlock), b[k]);
+        }
+    };
+    if (kAhead && blockIdx.x < p.rows) ask_row(blockIdx.x);
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        asm volatile("" : "+v"(t));                                             // addresses are formed in each row, not held
         const float rstd = p.rstd[row];
         const T *dy = (const T *)p.dy + row * p.n, *h = (const T *)p.h + row * p.n;
         double s = 0.0;
-        for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
-            Eight<T> a, b;
-            Eight<W> w;
-            ask8<false, false>(dy, p.n, 8 * u, a);
-            ask8<false, false>(h, p.n, 8 * u, b);
-            ask8<false, false>((const W *)p.weight, p.n, 8 * u, w);
-            settle8<false>(p.n, 8 * u, a);
-            settle8<false>(p.n, 8 * u, b);
-            settle8<false>(p.n, 8 * u, w);
-            f32x4 d[2] = {dw[2 * u], dw[2 * u + 1]};
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) {
+            if (first + k * kLongBlock >= p.units) continue;                    // the whole wave
+            const int c = 8 * (t + k * kLongBlock), at = kAhead ? k : 0, wk = kHoldW ? k : 0;
+            if (kHoldW) forget(w[wk]);
+            else ask8<false, false>((const W *)p.weight, p.n, c, w[wk]);
+            if (!kAhead) {
+                ask8<true, false>(dy, p.n, c, a[at]);
+                ask8<kKeepH, false>(h, p.n, c, b[at]);
+            }
+            settle8<false>(p.n, c, a[at]);
+            settle8<false>(p.n, c, b[at]);
+            if (!kHoldW) settle8<false>(p.n, c, w[wk]);
+            keep(k * kPer, a[at]);
+            if (kKeepH) keep(k * kPer + kChunks, b[at]);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float xh = b.f(i) * rstd;
-                s = __builtin_fma((double)(a.f(i) * w.f(i)), (double)xh, s);
-                d[i / 4][i % 4] += a.f(i) * xh;
+                const float xh = b[at].f(i) * rstd;
+                s = __builtin_fma((double)(a[at].f(i) * w[wk].f(i)), (double)xh, s);
+                dw[k][i] = __builtin_fma((double)a[at].f(i), (double)xh, dw[k][i]);
             }
-            dw[2 * u] = d[0];
-            dw[2 * u + 1] = d[1];
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (kAhead) ask_row(min(row + (int64_t)gridDim.x, p.rows - 1));        // past the last row that one again, not used
         const float mean = (float)(team_sum<kWaves>(s, sums[turn]) * p.per_n);
-        for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
-            const int left = p.n - 8 * u;
-            Eight<T> a, b, c;
-            Eight<W> w;
-            ask8<true, false>(dy, p.n, 8 * u, a);
-            ask8<true, false>(h, p.n, 8 * u, b);
-            ask8<false, false>((const W *)p.weight, p.n, 8 * u, w);
-            if (p.dsum) ask8<true, false>((const T *)p.dsum + row * p.n, p.n, 8 * u, c);
-            settle8<false>(p.n, 8 * u, a);
-            settle8<false>(p.n, 8 * u, b);
-            settle8<false>(p.n, 8 * u, w);
-            if (p.dsum) settle8<false>(p.n, 8 * u, c);
+        auto second = [&](int k, Eight<W> &w) {
+            const int u = t + k * kLongBlock, left = p.n - 8 * u;
+            Eight<T> y, x, ds;
+            if (!kKeepH) ask8<true, false>(h, p.n, 8 * u, x);
+            if (kHoldW) forget(w);
+            else ask8<false, false>((const W *)p.weight, p.n, 8 * u, w);
+            if (p.dsum) ask8<true, false>((const T *)p.dsum + row * p.n, p.n, 8 * u, ds);
+            recall(k * kPer, y);
+            if (kKeepH) recall(k * kPer + kChunks, x);
+            else settle8<false>(p.n, 8 * u, x);
+            if (!kHoldW) settle8<false>(p.n, 8 * u, w);
+            if (p.dsum) settle8<false>(p.n, 8 * u, ds);
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                v[i] = rstd * (a.f(i) * w.f(i) - (b.f(i) * rstd) * mean);
-                if (p.dsum) v[i] = c.f(i) + v[i];
+                v[i] = rstd * (y.f(i) * w.f(i) - (x.f(i) * rstd) * mean);
+                if (p.dsum) v[i] = ds.f(i) + v[i];
             }
             if (p.dres_out) store8((T *)p.dres_out + row * p.n + 8 * u, left, v);
             const uint64_t g = p.drop.first + 8 * ((uint64_t)row * p.units + u);
             if (p.draws == 32) drop8<false>(p.drop, g, v);
             if (p.draws == 16) drop8<true>(p.drop, g, v);
             store8((T *)p.dx_out + row * p.n + 8 * u, left, v);
+        };
+        if (kHoldW) {
+#pragma unroll
+            for (int k = 0; k < STEPS; k++)
+                if (first + k * kLongBlock < p.units) second(k, w[kHoldW ? k : 0]);
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < STEPS && first + k * kLongBlock < p.units; k++) second(k, w[0]);
         }
     }
     if (!p.parts) return;
-    f32x4 *part = reinterpret_cast<f32x4 *>(p.parts + (int64_t)blockIdx.x * p.units * 8);
-    for (int u = threadIdx.x; u < p.units; u += kLongBlock) {
-        part[2 * u] = dw[2 * u];
-        part[2 * u + 1] = dw[2 * u + 1];
+    float *part = p.parts + (int64_t)blockIdx.x * p.units * 8;
+#pragma unroll
+    for (int k = 0; k < STEPS; k++) {
+        const int u = threadIdx.x + k * kLongBlock;
+        if (u < p.units) store_part(part + 8 * u, dw[k]);
     }
 }
 
@@ -387,21 +449,29 @@ constexpr int kSumColumns = 32, kSumLanes = kSumColumns / 4, kSlices = 256 / kSu
 __global__ void __launch_bounds__(256)
 weight_sum_kernel(const float *parts, int count, int n, int pitch, float *dweight)
 {
-    __shared__ f32x4 slices[kSlices][kSumLanes];
+    __shared__ double slices[kSlices][kSumColumns];
     const int c4 = threadIdx.x % kSumLanes, slice = threadIdx.x / kSumLanes, c = blockIdx.x * kSumColumns + 4 * c4;
-    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (c < pitch) {
-#pragma unroll 8
-        for (int i = slice; i < count; i += kSlices) s += *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * pitch + c);
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    const float *from = parts + (c < pitch ? c : 0);
+    for (int i = slice; i < count; i += 8 * kSlices) {
+        f32x4 v[8];                                                            // asked for together
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[k] = *reinterpret_cast<const f32x4 *>(from + (int64_t)min(i + k * kSlices, count - 1) * pitch);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) s[j] += i + k * kSlices < count ? (double)v[k][j] : 0.0;
     }
-    slices[slice][c4] = s;
+#pragma unroll
+    for (int j = 0; j < 4; j++) slices[slice][4 * c4 + j] = s[j];
     __syncthreads();
     const int column = blockIdx.x * kSumColumns + threadIdx.x;
     if (threadIdx.x >= kSumColumns || column >= n) return;
-    float t = 0.0f;
+    double t = 0.0;
 #pragma unroll
-    for (int i = 0; i < kSlices; i++) t += slices[i][threadIdx.x / 4][threadIdx.x % 4];
-    dweight[column] = t;
+    for (int i = 0; i < kSlices; i++) t += slices[i][threadIdx.x];
+    dweight[column] = (float)t;
 }
 
 static gq_status check_norm(int64_t rows, int64_t n, int dtype, int weight_dtype, const gq_dropout_params *drop)
@@ -442,10 +512,12 @@ template <typename F> static gq_status with_team(int64_t rows, int64_t n, F &&f)
 }
 
 constexpr int64_t kManyRows = 2048;
+constexpr int64_t kMostHeld = 8192;       // columns that the registers of a team hold in the backward pass
 static bool four_teams(int64_t rows, int64_t n) { return n > 1024 && n <= 2048 && rows >= kManyRows; }
 
 // f(waves per row, steps, teams a workgroup, fewer than eight columns) for the backward pass, whose rows come with twice the registers;
-// none for rows of more than 16384 columns.  Teams of four waves: one a workgroup for few rows, four, with one part of the weight's
+// for rows of up to kMostHeld columns.  Above 6144 columns 16 waves of one step and 8 of two take: 8192x8192 bf16 74.3 and 77.8 us, with dropout
+// 117 and 139, with dsum 93 and 90; 4096x7000 41 and 50.  Teams of four waves: one a workgroup for few rows, four, with one part of the weight's
 // gradient between them, for many.  us with one and four: 300x2047 bf16 7.7, 8.5; 1000x2047 fp32 11.1, 13.7;
 // 1500x2047 13.5, 15.6, 2048x2047 17.3, 17.6; bf16 4096x2047 22.8, 18.4; with dropout 2048x2048 15.9, 12.5, 16384x2048 70.5, 61.3.
 template <typename F> static gq_status with_backward_team(int64_t rows, int64_t n, F &&f)
@@ -460,18 +532,18 @@ template <typename F> static gq_status with_backward_team(int64_t rows, int64_t 
     if (n <= 2048) return four_teams(rows, n) ? f(four, one, four, no) : f(four, one, one, no);
     if (n <= 4096) return f(integral_constant<int, 8>(), integral_constant<int, 1>(), one, no);
     if (n <= 6144) return f(integral_constant<int, 12>(), integral_constant<int, 1>(), one, no);
-    if (n <= 8192) return f(integral_constant<int, 8>(), integral_constant<int, 2>(), one, no);
-    return f(integral_constant<int, 16>(), integral_constant<int, 2>(), one, no);
+    return f(integral_constant<int, 16>(), one, one, no);
 }
 
 // Workgroups of the backward pass, each of which leaves one part of the weight's gradient: one a compute unit where it has enough
 // waves of its own and asks ahead, else two.  bf16, us with 256 and 512: 8192x4096 47.8 and 51.8, with dropout (more arithmetic, and
-// no asking ahead) 74.6 and 64.3; of one team of four waves each 1000x2047 fp32 11.3 and 12.0: too few rows each to make up for the parts.
+// no asking ahead) 71.6 and 64.0, but of 12 waves, of which two no longer fit, 8192x6000 95 and 112; of one team of four waves each
+// 1000x2047 fp32 11.3 and 12.0: too few rows each to make up for the parts.
 constexpr int64_t kMostParts = 512;
 static int64_t backward_groups(int64_t rows, int64_t n, bool drop)
 {
     const int64_t teams = n <= 1024 || four_teams(rows, n) ? (rows + 3) / 4 : rows;
-    const bool two = (n <= 512 || (drop && n <= 16384 && (n <= 1024 || n > 2048))) && teams >= 4 * kMostParts;
+    const bool two = (n <= 512 || (drop && n <= 4096 && (n <= 1024 || n > 2048))) && teams >= 4 * kMostParts;
     const int64_t most = two ? kMostParts : kMostParts / 2;
     return teams < 1 ? 1 : teams < most ? teams : most;
 }
@@ -537,16 +609,19 @@ gq_status gq_rms_norm_backward(const void *dy, const void *h, const void *dsum, 
         const gq_status launch = with_types(dtype, weight_dtype, [&](auto t, auto w) {
             typedef decltype(t) T;
             typedef decltype(w) W;
-            if (n > 16384) {
-                rms_norm_backward_long_kernel<T, W><<<(unsigned)groups, kLongBlock, 32 * (unsigned)p.units, stream>>>(p);
+            if (n > kMostHeld) {
+                auto kernel = n > 2 * kMostHeld ? rms_norm_backward_long_kernel<T, W, 4> : rms_norm_backward_long_kernel<T, W, 2>;
+                kernel<<<(unsigned)groups, kLongBlock, kLongLds, stream>>>(p);
                 return launched();
             }
             return with_backward_team(rows, n, [&](auto wpr, auto steps, auto of, auto tiny) {
                 constexpr int WPR = decltype(wpr)::value, STEPS = decltype(steps)::value, TEAMS = decltype(of)::value;
-                constexpr bool TINY = decltype(tiny)::value, kAhead = WPR < 16;      // as far as the registers reach
+                constexpr bool TINY = decltype(tiny)::value;
                 auto with_dsum = [&](auto there) {
                     constexpr bool DSUM = decltype(there)::value;
-                    constexpr bool kTwo = kAhead && WPR != 4;          // where there may be two workgroups a compute unit, with dropout
+                    constexpr bool kTwo = WPR == 1 || WPR == 8;        // where there may be two workgroups a compute unit, with dropout
+                    // as far as the registers reach: with the next row of binary32 and dsum, 16 waves spill (4096x8192 105.4 us, 101.5 without)
+                    constexpr bool kAhead = !(WPR == 16 && DSUM && sizeof(T) == 4);
                     return kTwo && groups == kMostParts && drop ? rms_norm_backward_kernel<T, W, WPR, STEPS, TEAMS, TINY, DSUM, !kTwo && kAhead>
                                                                 : rms_norm_backward_kernel<T, W, WPR, STEPS, TEAMS, TINY, DSUM, kAhead>;
                 };

@@ -104,6 +104,90 @@ def test_products_of_large_finite_rows_are_numbers(m, group):
     close(y[sure], want[sure], tol[sure])
 
 
+# ---- the weight's gradient ------------------------------------------------------------------------------------------
+
+# rows of fewer than eight columns, every team of waves, rows that are read twice; in bfloat16 and binary32
+TEAMS = [5, 64, 512, 900, 1500, 2500, 5003, 7001, 8193, 12_000, 16_384, 16_385, 20_001, 32_768]
+
+
+@gpu
+@pytest.mark.parametrize("drops", [False, True])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n", TEAMS)
+def test_weight_gradient_of_many_rows_keeps_small_terms(n, name, drops):
+    """One row of 2^24 and ones in all others: a sum in binary32 that met the large row first would lose the ones behind it."""
+    t, rows = TYPES[name], 60_000 if n < 1000 else 8000 if n < 3000 else 4100 if n < 16_385 else 2600
+    h = torch.ones(rows, n, dtype=t, device=DEV)
+    dy, dx = torch.ones_like(h), torch.empty_like(h)
+    dy[0] = 2.0 ** 24
+    dw, one = torch.empty(n, device=DEV), torch.ones(rows, device=DEV)
+    drop = gq.make_dropout(0.1, 5) if drops else None
+    gq.rms_norm_backward(dy, h, torch.ones(n, dtype=t, device=DEV), one, dx, dweight_out=dw, drop=drop)
+    want = torch.full((n,), 2.0 ** 24 + rows - 1, dtype=torch.float64)
+    # h rstd and the products are exact; a part of the sum and the sum are rounded once each
+    close(dw, want, 2 * U * want)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 300, 1000, 2100, 9000])
+@pytest.mark.parametrize("n", TEAMS)
+def test_weight_gradient_is_rounded_no_more_often_with_more_rows(n, rows):
+    if rows * n > 40_000_000:
+        rows = 40_000_000 // n
+    g = torch.Generator(DEV).manual_seed(n + rows)
+    h, dy = (torch.randn(rows, n, generator=g, device=DEV) for _ in range(2))
+    rstd = (1.0 / torch.sqrt(h.double().square().mean(1) + 1e-5)).float()
+    dw, again, dx = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty_like(h)
+    ws = torch.full((gq.rms_norm_workspace_bytes(rows, n),), 0xFF, dtype=torch.uint8, device=DEV)      # NaN where nothing is written
+    w = torch.randn(n, generator=g, device=DEV)
+    gq.rms_norm_backward(dy, h, w, rstd, dx, dweight_out=dw, workspace=ws)
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    # h rstd, a part, and the sum
+    close(dw, terms.sum(0), 1.01 * U * (2 * terms.abs().sum(0) + terms.sum(0).abs()))
+    gq.rms_norm_backward(dy, h, w, rstd, dx, dweight_out=again)
+    assert torch.equal(again, dw)
+
+
+# ---- rows that the registers do not hold, and the longest that they do: more rows than workgroups ---------------------
+
+@gpu
+@pytest.mark.parametrize("draws", [0, 16, 32])
+@pytest.mark.parametrize("with_dsum", [False, True])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [8200, 12_001, 16_384, 16_385, 20_001, 32_768])
+def test_rms_norm_backward_of_many_long_rows(n, name, with_dsum, draws):
+    rows, t = 1100 if name == "bf16" else 600, TYPES[name]
+    g = torch.Generator(DEV).manual_seed(n + draws)
+    h, dy, ds = (torch.randn(rows, n, generator=g, device=DEV).to(t) for _ in range(3))
+    w = torch.randn(n, generator=g, device=DEV).to(t)
+    ds = ds if with_dsum else None
+    rstd = (1.0 / torch.sqrt(h.double().square().mean(1) + 1e-5)).float()
+    make = lambda first: gq.make_dropout(0.25, L.SEED, 2, 8 * math.ceil(n / 8) * first, draws) if draws else None     # noqa: E731
+    dx, dres, dw = L.Guarded((rows, n), t), L.Guarded((rows, n), t), L.Guarded((n,), torch.float32)
+    gq.rms_norm_backward(dy, h, w, rstd, dx.t, dsum=ds, dres_out=dres.t if draws else None, dweight_out=dw.t, drop=make(0))
+    assert dx.intact() and dres.intact() and dw.intact()
+    for a, b in ((0, 3), (254, 260), (510, 516), (rows - 5, rows)):     # a few of the rows in 64 bits, and in a call of their own
+        xh, gr = h[a:b].double() * rstd[a:b].double()[:, None], dy[a:b].double() * w.double()
+        c, ca = (gr * xh).mean(1, keepdim=True), (gr * xh).abs().mean(1, keepdim=True)
+        dh = rstd[a:b].double()[:, None] * (gr - xh * c)
+        tol = U * rstd[a:b].double()[:, None] * (3 * gr.abs() + xh.abs() * (3 * c.abs() + 2 * ca) + 2 * (gr - xh * c).abs()) * 1.01
+        if with_dsum:
+            dh = ds[a:b].double() + dh
+            tol = tol + U * (dh.abs() + tol)
+        got = dres.t if draws else dx.t
+        close(got[a:b], dh, tol + L.half_step(t) * (dh.abs() + tol) + L.least(t))
+        px, pres = torch.empty(b - a, n, dtype=t, device=DEV), torch.empty(b - a, n, dtype=t, device=DEV)
+        gq.rms_norm_backward(dy[a:b].clone(), h[a:b].clone(), w, rstd[a:b].clone(), px, dsum=None if ds is None else ds[a:b].clone(),
+                             dres_out=pres if draws else None, drop=make(a))
+        assert torch.equal(px, dx.t[a:b]) and (not draws or torch.equal(pres, dres.t[a:b]))
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    close(dw.t, terms.sum(0), 1.01 * U * (2 * terms.abs().sum(0) + terms.sum(0).abs()))
+    again = torch.empty(n, device=DEV)
+    if ds is not None:                                                # over dy and dsum
+        gq.rms_norm_backward(dy, h, w, rstd, dy, dsum=ds, dres_out=ds if draws else None, dweight_out=again, drop=make(0))
+        assert torch.equal(dy, dx.t) and (not draws or torch.equal(ds, dres.t)) and torch.equal(again, dw.t)
+
+
 # ---- callers ----------------------------------------------------------------------------------------------------------
 
 def test_backward_refuses_what_is_no_matrix_like_the_other_calls():
