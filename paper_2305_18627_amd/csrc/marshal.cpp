@@ -485,6 +485,17 @@ struct DropParams {                                                    // a ctyp
     const gq_dropout_params *get() const { return there ? reinterpret_cast<const gq_dropout_params *>(view.buf) : nullptr; }
 };
 
+// A call that writes these tensors (None: not asked for).  Autograd is told, as by torch's own operations: a backward pass that kept one of them
+// refuses instead of computing with what was written over it.
+template <typename F> PyObject *writing(std::initializer_list<PyObject *> outputs, F &&f)
+{
+    PyObject *st = call(f);
+    if (st && PyLong_AsLong(st) == (long)GQ_OK)
+        for (PyObject *o : outputs)
+            if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+    return st;
+}
+
 // x, drop, out, residual, stream
 PyObject *dropout(PyObject *const *a)
 {
@@ -494,7 +505,7 @@ PyObject *dropout(PyObject *const *a)
     const gq_dtype t = dtype_of(x, "x");
     void *out = given(a[2], s.numel(), x.scalar_type(), "out"), *res = sized(a[3], s.numel(), x.scalar_type(), "residual");
     void *xp = x.data_ptr(), *st = stream_for(a[4], {a[0], a[2], a[3]});
-    return call([&] { return lib.gq_dropout_(xp, res, s.rows, s.n, t, p.get(), out, st); });
+    return writing({a[2]}, [&] { return lib.gq_dropout_(xp, res, s.rows, s.n, t, p.get(), out, st); });
 }
 
 // x, weight, eps, out, residual, sum_out, scales_out, rstd_out, drop, stream
@@ -510,7 +521,7 @@ PyObject *rms_norm(PyObject *const *a)
     void *res = sized(a[4], s.numel(), x.scalar_type(), "residual"), *sum = sized(a[5], s.numel(), x.scalar_type(), "sum_out");
     void *scales = sized(a[6], s.rows, at::kFloat, "scales_out"), *rstd = sized(a[7], s.rows, at::kFloat, "rstd_out");
     void *xp = x.data_ptr(), *wp = w.data_ptr(), *op = o.data_ptr(), *st = stream_for(a[9], {a[0], a[1], a[3], a[4], a[5], a[6], a[7]});
-    return call([&] {
+    return writing({a[3], a[5], a[6], a[7]}, [&] {
         return lib.gq_rms_norm_(xp, res, s.rows, s.n, t, wp, wt, (float)eps, p.get(), sum, op, ot, (float *)scales, (float *)rstd, st);
     });
 }
@@ -534,7 +545,7 @@ PyObject *rms_norm_backward(PyObject *const *a)
         bytes = (size_t)(u.numel() * (int64_t)u.element_size());
     }
     void *yp = dy.data_ptr(), *wp = w.data_ptr(), *st = stream_for(a[10], {a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[9]});
-    return call([&] {
+    return writing({a[4], a[6], a[7], a[9]}, [&] {
         return lib.gq_rms_norm_backward_(yp, h, dsum, s.rows, s.n, t, wp, wt, (const float *)rstd, p.get(), dres, dx, (float *)dw, ws, bytes, st);
     });
 }
@@ -569,7 +580,7 @@ PyObject *group_quantize(PyObject *const *a)
     const Weights out(a[2], a[3], a[1], s.n);
     if (out.rows != s.rows) refuse("w and codes_out differ in rows");
     void *wp = w.data_ptr(), *st = stream_for(a[4], {a[0], a[2], a[3]});
-    return call([&] { return lib.gq_group_quantize_(wp, s.rows, s.n, t, out.group, out.codes, out.scales, out.type, st); });
+    return writing({a[2], a[3]}, [&] { return lib.gq_group_quantize_(wp, s.rows, s.n, t, out.group, out.codes, out.scales, out.type, st); });
 }
 
 // codes, scales, group, out, stream
@@ -581,7 +592,7 @@ PyObject *group_dequantize(PyObject *const *a)
     const Weights in(a[0], a[1], a[2], s.n);
     if (in.rows != s.rows) refuse("codes and out differ in rows");
     void *op = o.data_ptr(), *st = stream_for(a[4], {a[0], a[1], a[3]});
-    return call([&] { return lib.gq_group_dequantize_(in.codes, in.scales, in.type, s.rows, s.n, in.group, op, t, st); });
+    return writing({a[3]}, [&] { return lib.gq_group_dequantize_(in.codes, in.scales, in.type, s.rows, s.n, in.group, op, t, st); });
 }
 
 // x, codes, scales, group, out, x_scales, bias, stream
@@ -594,7 +605,7 @@ PyObject *w4_matvec(PyObject *const *a)
     if (so.rows != s.rows || so.n != w.rows) refuse("out must be the rows of x by the rows of the weights");
     void *xs = sized(a[5], s.rows, at::kFloat, "x_scales"), *bias = sized(a[6], w.rows, y.scalar_type(), "bias");
     void *xp = x.data_ptr(), *yp = y.data_ptr(), *st = stream_for(a[7], {a[0], a[1], a[2], a[4], a[5], a[6]});
-    return call([&] {
+    return writing({a[4]}, [&] {
         return lib.gq_w4_matvec_(xp, (const float *)xs, s.rows, t, w.codes, w.scales, w.type, w.rows, s.n, w.group, bias, yp, yt, st);
     });
 }

@@ -190,6 +190,49 @@ def test_rms_norm_backward_of_many_long_rows(n, name, with_dsum, draws):
 
 # ---- callers ----------------------------------------------------------------------------------------------------------
 
+@gpu
+def test_autograd_sees_what_is_written():
+    """A tensor that autograd keeps for its backward pass and a call writes over: the backward pass refuses, as for torch's own operations."""
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device=DEV)                     # noqa: E731
+    drop, w = gq.make_dropout(0.1, 1), torch.ones(8, device=DEV)
+    codes, scales = z(4, 16, t=torch.uint8), torch.ones(4, 1, device=DEV)
+    gq.group_quantize(torch.randn(4, 8, device=DEV), 32, codes, scales)
+    calls = {"dropout": lambda o: gq.dropout(z(4, 8), drop, o),
+             "dropout over the residual": lambda o: gq.dropout(z(4, 8), drop, o, residual=o),
+             "norm": lambda o: gq.rms_norm(z(4, 8), w, 1e-5, o),
+             "sum": lambda o: gq.rms_norm(z(4, 8), w, 1e-5, z(4, 8), residual=o, sum_out=o),
+             "backward": lambda o: gq.rms_norm_backward(z(4, 8), z(4, 8), w, z(4), o),
+             "the residual's gradient": lambda o: gq.rms_norm_backward(z(4, 8), z(4, 8), w, z(4), z(4, 8), dres_out=o, drop=drop),
+             "unfolded": lambda o: gq.group_dequantize(codes, scales, 32, o)}
+    for what, call in calls.items():
+        leaf = torch.randn(4, 8, device=DEV, requires_grad=True)
+        kept = leaf * 2.0
+        loss = (kept * kept).sum()
+        call(kept.detach())                                           # shares memory and version with what autograd keeps
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+    vectors = {"rstd_out": lambda o: gq.rms_norm(z(4, 8), w, 1e-5, z(4, 8), rstd_out=o),
+               "scales_out": lambda o: gq.rms_norm(z(4, 8), w, 1e-5, z(4, 8, t=torch.int8), scales_out=o),
+               "product": lambda o: gq.w4_matvec(z(1, 8, t=torch.bfloat16), codes, scales, 32, o.view(1, 4)),
+               "scales": lambda o: gq.group_quantize(z(4, 8), 32, codes, o.view(4, 1))}
+    for what, call in vectors.items():
+        o = z(4)
+        before = o._version
+        call(o)
+        assert o._version == before + 1, what
+    o, before = z(8), codes._version
+    gq.rms_norm_backward(z(4, 8), z(4, 8), w, z(4), z(4, 8), dweight_out=o)
+    assert o._version == 1
+    gq.group_quantize(z(4, 8), 32, codes, scales)
+    assert codes._version == before + 1
+    x = z(4, 8)
+    with pytest.raises(gq.GQError):                                   # a call that is refused has written nothing
+        gq.rms_norm(z(4, 8), w, -1.0, x)
+    assert x._version == 0 and w._version == 0
+    with torch.inference_mode():                                      # such tensors have no version
+        gq.dropout(z(4, 8), drop, z(4, 8))
+
+
 def test_backward_refuses_what_is_no_matrix_like_the_other_calls():
     x, w = torch.zeros(2, 8), torch.zeros(8)
     with pytest.raises(TypeError):
