@@ -214,6 +214,53 @@ def test_rms_norm_backward_of_many_long_rows(n, name, with_dsum, draws):
         assert torch.equal(dy, dx.t) and (not draws or torch.equal(ds, dres.t)) and torch.equal(again, dw.t)
 
 
+# ---- long launches of every type --------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows,n", [(4200, 4096), (4100, 4104), (4100, 4099), (1, 17_000_003)])
+def test_long_dropouts_of_every_type(rows, n, name):
+    t = TYPES[name]
+    x = torch.randn(rows, n, device=DEV).to(t)
+    res, whole, pitch = torch.randn(rows, n, device=DEV).to(t), L.Guarded((rows, n), t), 8 * math.ceil(n / 8)
+    for bits in (32, 16):
+        for r in (None, res):
+            gq.dropout(x, gq.make_dropout(0.4, 9, 1, 16, bits), whole.t, residual=r)
+            assert whole.intact()
+            for a, b in ((0, 8), (rows // 2, rows // 2 + 8), (rows - 8, rows)) if rows > 1 else ((0, 8000), (8_000_000, 8_008_000), (n - 8003, n)):
+                part = (slice(a, b), slice(0, n)) if rows > 1 else (slice(0, 1), slice(a, b))
+                drop = gq.make_dropout(0.4, 9, 1, 16 + (pitch * a if rows > 1 else a), bits)
+                k, by = L.kept(b - a if rows > 1 else 1, n if rows > 1 else b - a, drop)
+                v = torch.where(k, x[part].double().cpu() * by, 0.0)
+                want = v if r is None else r[part].double().cpu() + v
+                close(whole.t[part], want, 2 * U * v.abs() + (U + L.half_step(t)) * (want.abs() + 2 * U * v.abs()) + L.least(t))
+
+
+@gpu
+@pytest.mark.parametrize("scale", ["f32", "bf16"])
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,cols", [(4200, 4096), (4100, 4104), (4100, 4099), (8200, 2047)])
+def test_long_weights_of_every_type(rows, cols, group, name, scale):
+    """Whole groups a row, and ragged ones; a few of the rows against the definition."""
+    t, st, G = TYPES[name], TYPES[scale], -(-cols // group)
+    w = (torch.randn(rows, cols, device=DEV) * 0.02).to(t)
+    codes, scales, out = L.Guarded((rows, gq.w4_row_bytes(cols)), torch.uint8), L.Guarded((rows, G), st), L.Guarded((rows, cols), t)
+    gq.group_quantize(w, group, codes.t, scales.t)
+    gq.group_dequantize(codes.t, scales.t, group, out.t)
+    assert codes.intact() and scales.intact() and out.intact()
+    for a, b in ((0, 20), (rows // 2, rows // 2 + 20), (rows - 20, rows)):
+        part = w[a:b].cpu()
+        padded = torch.nn.functional.pad(part, (0, G * group - cols)).reshape(b - a, G, group)
+        want = (padded.float().abs().amax(2) * torch.tensor(1.0 / 7.0)).to(st)
+        assert torch.equal(scales.t[a:b].cpu(), want)
+        s = L.per_column(want, cols, group)
+        q = L.unpacked(codes.t[a:b], cols)
+        assert torch.equal(q[:, :cols], (part.double() / s).round().clamp(-7, 7).long()) and not q[:, cols:].any()
+        value = q[:, :cols].double() * s
+        close(out.t[a:b], value, (U + L.half_step(t)) * value.abs() + L.least(t))
+
+
 # ---- callers ----------------------------------------------------------------------------------------------------------
 
 @gpu
