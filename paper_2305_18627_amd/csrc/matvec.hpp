@@ -448,19 +448,21 @@ static gq_status launch_matvec(const MatvecArgs &p, hipStream_t stream)
     return launched();
 }
 
-// Which shape of workgroup.  Few rows of x stay in LDS.  us, bf16, groups of 128, 1 row of x; WK waves that take U chunks each:
-//   4096x4096   16 waves of 1 chunk 4.6, 8 of 2 5.0, 8 of 4 5.1  (too few tiles for more than one workgroup a compute unit)
-//   14336x4096  4 of 4 9.1, 8 of 4 9.4, 8 of 2 10.5;  4 rows of x: 12.1, 11.0, 11.0
-//   28672x8192  8 of 2 26.6, 4 of 4 26.9, 8 of 4 27.1
+// Which shape of workgroup.  Few rows of x stay in LDS.  us, bf16, groups of 128; WK waves that take U chunks each:
+//   1 row of x    4096x4096  16 waves of 1 chunk 4.8, 8 of 2 5.3, 4 of 4 5.3  (too few tiles for more than one workgroup a compute unit)
+//                14336x4096  4 of 4 9.4, 8 of 2 9.7, 16 of 1 12.7;  2 rows of x: 10.8, 9.6, 13.6;  4: 12.5, 11.0, 11.7
+//                28672x8192  8 of 2 25.9, 4 of 4 28.3, 16 of 1 32.7
 //   8 rows of x, 14336x4096: 512 workgroups 13.4, 768: 18
-// Otherwise as many rows of weights a workgroup (they share its staged x) as leave about one workgroup a compute unit, and as many
-// waves to share out the columns as fill it.  us, 16 | 32 | 64 rows of x, by the rows of weights a workgroup:
-//   4096x4096   16: 6.9, 32: 8.5, 64: 12.2         |  slices of 16 of x, 32: 8.6, of 32: 12.2           |  slices of 32, 32: 12.3, 64: 14.7
-//   8192x8192   32: 17.5, 64: 24.4, 16: 24.7       |  slices of 16, 64: 24.2, of 32, 32: 25.2, 64: 29.4 |  slices of 32, 64: 30.0, 32: 45.8
-//   14336x4096  64: 14.2, 32: 15.5                 |  64: 17.0, 32: 19.6                                |  slices of 32, 128: 26.0, of 64, 64: 26.8
-//   28672x8192  64 (8 waves): 38.2, 128: 46.3, 64 (16 waves): 48.5  |  64 (8 waves): 50.1, 128: 51.7    |  128: 72.3, slices of 32, 128: 93.7
-// (taken with codes one step ahead; the first of each now: 6.3, 8.9, 12.3; 16.8, 22.8, 26.9; 13.7, 17.0, 23.7; 39.8, 50.7, 68.  With them two ahead
-// 32 rows of x take 128 rows a workgroup from 1024 tiles on: 17000x4096 22.6, with 64 24.1, 20000x8192 42.3, 47.2, 28672x8192 46.8, 50.0)
+// Otherwise as many rows of weights a workgroup (they share its staged x) as leave no more than one workgroup a compute unit, 256 in all, and as
+// many waves to share out the columns as fill it: one workgroup more starts a second round.  us, 16 | 32 | 64 rows of x, by the rows of
+// weights a workgroup (and the rows of x in its slice, where that is less):
+//   4096x4096    16: 6.6, 32: 9.2, 64: 12.1   |  32 (16) 9.6, 16 (16) 11.4, 32 12.3        |  32 (32) 12.7, 64 (32) 14.4, 32 (16) 17.7
+//   5120x4096    32: 9.3, 16: 11.1, 64: 12.2  |  32: 12.4, 64 14.3, 32 (16) 16.9           |  64 (32) 14.2, 128 (32) 20.1, 32 (32) 22.1
+//   8192x8192    32: 17.2, 64: 21.8, 16: 22.6 |  32: 23.3, 64 (16) 22.2, 64 26.0           |  64 (32) 26.5, 128 (32) 40.0, 32 (32) 42.3
+//   10240x4096   64: 13.1, 32: 17.7, 16: 18.5 |  64: 15.4, 128 21.9, 32 24.7               |  128 (32) 22.1, 64 (32) 27.9, 128 34.2
+//   16384x4096   64: 13.8, 64 (8 waves) 14.7, 32: 19.2  |  64: 17.7, 128 22.6, 32 26.5     |  128 (32) 24.0, 64 (32) 31.2, 128 36.2
+//   18000x4096   64 (8 waves) 19.5, 64 24.8, 32: 26.1   |  128: 22.9, 64 29.5              |  128: 35.7, 128 (32) 42.5, 64 (32) 42.8
+//   28672x8192   64 (8 waves) 38.7, 64 43.6, 32: 58.3   |  128: 46.0, 64 53.3              |  128: 71.7, 128 (32) 82.8, 64 (32) 98.1
 template <typename X, typename S, int GROUP> static gq_status matvec_of_group(MatvecArgs p, hipStream_t stream)
 {
     const int64_t tiles = (p.rows + 15) / 16;
@@ -469,11 +471,11 @@ template <typename X, typename S, int GROUP> static gq_status matvec_of_group(Ma
         while ((1 << p.row_shift) < p.cols) p.row_shift++;
         if (((int64_t)p.m << p.row_shift) * (int)sizeof(X) <= 64 * 1024)
             return tiles <= 256 ? launch_matvec<X, S, GROUP, 1, 1, 16, 1, true>(p, stream)
-                   : tiles > 512 && tiles <= 1024 && p.m <= 2 ? launch_matvec<X, S, GROUP, 1, 1, 4, 4, true>(p, stream)
+                   : tiles > 512 && tiles <= 1024 && p.m == 1 ? launch_matvec<X, S, GROUP, 1, 1, 4, 4, true>(p, stream)
                                                               : launch_matvec<X, S, GROUP, 1, 1, 8, 2, true>(p, stream);
     }
     const int64_t work = tiles * ((p.m + 63) / 64);                                // of more than 64 rows of x, slices of 64 or 32
-    const int size = work <= 320 ? 0 : work <= 640 ? 1 : work <= 1024 ? 2 : 3;
+    const int size = work <= 256 ? 0 : work <= 512 ? 1 : work <= 1024 ? 2 : 3;
     if (p.m <= 16)
         return size == 0   ? launch_matvec<X, S, GROUP, 1, 1, 8, 2, false>(p, stream)
                : size == 1 ? launch_matvec<X, S, GROUP, 1, 2, 8, 2, false>(p, stream)
