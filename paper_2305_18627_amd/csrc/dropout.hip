@@ -9,44 +9,34 @@
 
 namespace gq {
 
-// Units a lane: 4 keep enough in flight in long launches, in short ones more lanes do (bf16, 32 bits: 16384x8192 110, 94 and 90 us with 1, 2
-// and 4; 2048x4096 7.7, 7.9, 7.5; 512x4096 3.2, 3.5, 4.0; 1x100003 2.1, 2.5, 3.3).
-constexpr int64_t kLongDropout = 1 << 21;
-
-// out = residual + (draw < t ? 0 : x scale).  A lane owns UNITS units, each of eight columns of one row and one (16 bits) or two (32 bits)
-// Philox calls.  All loads are asked for before the first draw, so that the calls' arithmetic runs under their latency.
-// Bound by memory where draws have 16 bits (16384x8192 bf16 with a residual: 128 us, 6.3 TB/s), by memory and the calls' products
-// together with 32 (8192x8192 fp32 without one: 96 us, 5.6 TB/s); a short launch by its latency (100003 fp32: 2.4 us).
-template <typename T, bool SHORT, bool RESIDUAL, bool TINY, bool FLAT, int UNITS>
+// out = residual + (draw < t ? 0 : x scale).  A lane owns a unit of eight columns of one row and one (16 bits) or two (32 bits) Philox calls.
+// Both loads are asked for before the first draw, so that the calls' arithmetic runs under their latency.  Several units a lane keep
+// more in flight and are no faster, us with 1, 2 and 4: 16384x8192 bf16 with a residual 126, 132, 131, 8192x8192 bf16 43, 47, 48, fp32 95, 96, 97,
+// 4096x4096 bf16 12.2, 14.9, 14.2, 512x4096 3.0, 3.8, 4.1; only fp32 in odd rows without a residual gains a little (8001x8191 107, 103, 105).
+// Bound by memory: 16384x8192 bf16 with a residual 122 us, 6.6 TB/s, 8192x8192 fp32 without one 94, 5.7; a short launch by its latency
+// (100003 fp32: 2.0 us).
+template <typename T, bool SHORT, bool RESIDUAL, bool TINY, bool FLAT>
 __global__ void __launch_bounds__(kBlock)
 dropout_kernel(const T *x, const T *residual, T *out, int64_t rows, uint32_t per_row, int64_t n, Drop drop)
 {
-    RowUnit at[UNITS];
-    Eight<T> v[UNITS], r[UNITS];
+    const RowUnit at = row_unit<1, FLAT>(blockIdx.x, 0, per_row);
+    const int64_t row = FLAT ? 0 : at.row < rows ? at.row : rows - 1, c = (int64_t)at.unit * 8;
+    Eight<T> v, r;
+    ask8<true, TINY>(x + row * n, n, c, v);
+    if (RESIDUAL) ask8<true, TINY>(residual + row * n, n, c, r);
+    if (at.row >= rows) return;                                       // not before the loads, which would wait for it
+    uint32_t draw[8];
+    draws8<SHORT>(drop, drop.first + ((uint64_t)row * per_row + at.unit) * 8, draw);
+    __builtin_amdgcn_sched_barrier(0);                                // no wait for the loads above this
+    settle8<TINY>(n, c, v);
+    if (RESIDUAL) settle8<TINY>(n, c, r);
+    float f[8];
 #pragma unroll
-    for (int k = 0; k < UNITS; k++) {
-        at[k] = row_unit<UNITS, FLAT>(blockIdx.x, k, per_row);
-        const int64_t c = (int64_t)at[k].unit * 8, row = FLAT ? 0 : at[k].row < rows ? at[k].row : rows - 1;
-        ask8<true, TINY>(x + row * n, n, c, v[k]);
-        if (RESIDUAL) ask8<true, TINY>(residual + row * n, n, c, r[k]);
+    for (int i = 0; i < 8; i++) {
+        f[i] = dropped(drop, draw[i], v.f(i));
+        if (RESIDUAL) f[i] = r.f(i) + f[i];
     }
-#pragma unroll
-    for (int k = 0; k < UNITS; k++) {
-        if (at[k].row >= rows) return;
-        const int64_t c = (int64_t)at[k].unit * 8;
-        settle8<TINY>(n, c, v[k]);
-        if (RESIDUAL) settle8<TINY>(n, c, r[k]);
-        float f[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = v[k].f(i);
-        const int64_t row = FLAT ? 0 : at[k].row;
-        drop8<SHORT>(drop, drop.first + ((uint64_t)row * per_row + at[k].unit) * 8, f);
-        if (RESIDUAL) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) f[i] = r[k].f(i) + f[i];
-        }
-        store8(out + row * n + c, n - c, f);
-    }
+    store8(out + row * n + c, n - c, f);
 }
 
 }  // namespace gq
@@ -63,18 +53,15 @@ extern "C" gq_status gq_dropout(const void *x, const void *residual, int64_t row
     if (!aligned(x, 16) || !aligned(out, 16) || !aligned_or_null(residual, 16)) return GQ_ERR_INVALID_ARG;
     const bool flat = n >= 8 && (rows == 1 || n % 8 == 0) && flat_fits(rows * (pitch8(n) / 8));      // whole units a row
     if (flat) n *= rows, rows = 1;
-    const int64_t per_row = pitch8(n) / 8, units = rows * per_row;
-    const bool four = n >= 8 && units >= kLongDropout;
-    const int64_t per_block = (four ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
+    const int64_t per_row = pitch8(n) / 8, blocks = (rows * per_row + kBlock - 1) / kBlock;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     const Drop d = make_drop(p);
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         auto go = [&](auto shorter, auto with_residual) {
             constexpr bool SHORT = decltype(shorter)::value, RESIDUAL = decltype(with_residual)::value;
-            auto kernel = n < 8 ? dropout_kernel<T, SHORT, RESIDUAL, true, false, 1>
-                          : flat ? (four ? dropout_kernel<T, SHORT, RESIDUAL, false, true, 4> : dropout_kernel<T, SHORT, RESIDUAL, false, true, 1>)
-                                 : (four ? dropout_kernel<T, SHORT, RESIDUAL, false, false, 4> : dropout_kernel<T, SHORT, RESIDUAL, false, false, 1>);
+            auto kernel = n < 8 ? dropout_kernel<T, SHORT, RESIDUAL, true, false>
+                          : flat ? dropout_kernel<T, SHORT, RESIDUAL, false, true> : dropout_kernel<T, SHORT, RESIDUAL, false, false>;
             kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)x, (const T *)residual, (T *)out, rows, (uint32_t)per_row, n, d);
             return launched();
         };

@@ -139,10 +139,9 @@ struct Drop {
     float scale;          // of what is kept
 };
 
-// v[0..7], the elements g .. g + 7 of the stream (g a multiple of 4, of 8 with short draws), after dropout
-template <bool SHORT> __device__ __forceinline__ void drop8(const Drop &d, uint64_t g, float *v)
+// the draws of the elements g .. g + 7 of the stream (g a multiple of 4, of 8 with short draws)
+template <bool SHORT> __device__ __forceinline__ void draws8(const Drop &d, uint64_t g, uint32_t *r)
 {
-    uint32_t r[8];
     if (SHORT) {
         const uint64_t call = g >> 3;
         const Words4 w = philox4x32_10<false>((uint32_t)call, (uint32_t)(call >> 32), d.worker, 3u, d.k0, d.k1);
@@ -157,8 +156,15 @@ template <bool SHORT> __device__ __forceinline__ void drop8(const Drop &d, uint6
             for (int i = 0; i < 4; i++) r[4 * h + i] = w.w[i];
         }
     }
+}
+__device__ __forceinline__ float dropped(const Drop &d, uint32_t draw, float v) { return draw >= d.threshold ? v * d.scale : 0.0f; }
+// v[0..7], the elements g .. g + 7, after dropout
+template <bool SHORT> __device__ __forceinline__ void drop8(const Drop &d, uint64_t g, float *v)
+{
+    uint32_t r[8];
+    draws8<SHORT>(d, g, r);
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = r[i] >= d.threshold ? v[i] * d.scale : 0.0f;
+    for (int i = 0; i < 8; i++) v[i] = dropped(d, r[i], v[i]);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
