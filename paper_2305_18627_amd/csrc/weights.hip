@@ -136,12 +136,14 @@ group_dequantize_kernel(const uint32_t *codes, const S *scales, int64_t rows, in
 
 using namespace gq;
 
-// Units a lane: 4 keep enough in flight in long launches, in short ones more lanes do (quantise 8192x8192 bf16, with its scale still a division: 47.1, 44.9
-// and 43.7 us with 1, 2 and 4, unfold 35.1, 33.5, 32.0; 2048x4096: 8.1, 7.9, 9.4 and 5.8, 5.9, 6.7; 128x4096: 3.0, 3.8, 5.6 and 1.9, 2.1, 2.5).
-constexpr int64_t kLongWeights = 1 << 21;
+// Units a lane: more keep more in flight in long launches, in short ones more lanes do.  us with 1, 2 and 4, groups of 128:
+//   quantise  bf16  2048x4096 6.4, 6.7, 7.3   4096x4096 10.6, 11.3, 11.2   8192x8192 36.0, 35.6, 34.6   8001x8191 43.4, 40.3, 38.0
+//             fp32  2048x4096 9.1, 8.8, 9.3   4096x4096 15.2, 15.3, 15.5   8192x8192 53.5, 54.4, 54.8   8001x8191 52.6, 53.0, 55.2
+//   unfold    bf16  512x4096 2.5, 2.6, 2.9    2048x4096 5.4, 4.4, 4.3      8192x8192 34.8, 30.2, 30.8   8001x8191 37.4, 34.1, 34.3
+//             fp32  512x4096 3.4, 3.4, 3.5    2048x4096 10.6, 9.5, 8.4     8192x8192 63.5, 57.3, 55.0   8001x8191 71.0, 60.6, 66.1
+constexpr int64_t kLongQuantize = 1 << 21, kLongUnfold = 1 << 20;
 // rows of whole groups: codes and scales of a row end where the next one's begin, the matrix is one row
 static bool is_flat(int64_t rows, int64_t cols, int group) { return cols % group == 0 && flat_fits(rows * (cols / 4)); }
-static bool long_launch(int64_t units, int64_t cols) { return cols >= 8 && units >= kLongWeights; }
 
 extern "C" {
 
@@ -159,7 +161,8 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
     if (flat) cols *= rows, rows = 1;
     // whole groups of units, whole words of codes
     const int64_t row_words = (cols + 31) / 32 * 4, per_row = ((cols + group - 1) / group * group) / 8, units = rows * per_row;
-    const int64_t per_block = (long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
+    const bool four = cols >= 8 && dtype != GQ_F32 && units >= kLongQuantize;
+    const int64_t per_block = (four ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
@@ -167,10 +170,10 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
             typedef decltype(s) S;
             auto of_group = [&](auto g) {
                 constexpr int GROUP = decltype(g)::value;
-                const bool four = long_launch(units, cols);
+                constexpr int kFour = sizeof(T) == 2 ? 4 : 1;
                 return cols < 8 ? group_quantize_kernel<T, S, GROUP, true, false, 1>
-                       : flat ? (four ? group_quantize_kernel<T, S, GROUP, false, true, 4> : group_quantize_kernel<T, S, GROUP, false, true, 1>)
-                              : (four ? group_quantize_kernel<T, S, GROUP, false, false, 4> : group_quantize_kernel<T, S, GROUP, false, false, 1>);
+                       : flat ? (four ? group_quantize_kernel<T, S, GROUP, false, true, kFour> : group_quantize_kernel<T, S, GROUP, false, true, 1>)
+                              : (four ? group_quantize_kernel<T, S, GROUP, false, false, kFour> : group_quantize_kernel<T, S, GROUP, false, false, 1>);
             };
             auto kernel = group == 32 ? of_group(std::integral_constant<int, 32>())
                                       : group == 64 ? of_group(std::integral_constant<int, 64>()) : of_group(std::integral_constant<int, 128>());
@@ -192,13 +195,13 @@ gq_status gq_group_dequantize(const void *codes, const void *scales, gq_dtype sc
     const bool flat = is_flat(rows, cols, group);
     if (flat) cols *= rows, rows = 1;
     const int64_t row_words = (cols + 31) / 32 * 4, per = 16 / (int64_t)dtype_size(dtype), per_row = (cols + per - 1) / per, units = rows * per_row;
-    const int64_t per_block = (long_launch(units, cols) ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
+    const bool four = cols >= 8 && units >= kLongUnfold;
+    const int64_t per_block = (four ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
     if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         return with_scale_type(scale_dtype, [&](auto s) {
             typedef decltype(s) S;
-            const bool four = long_launch(units, cols);
             auto kernel = flat ? (four ? group_dequantize_kernel<T, S, true, 4> : group_dequantize_kernel<T, S, true, 1>)
                                : (four ? group_dequantize_kernel<T, S, false, 4> : group_dequantize_kernel<T, S, false, 1>);
             kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>(
