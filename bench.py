@@ -89,7 +89,8 @@ def profiled_traffic(path, version):
             return None, None, ("profiles/ holds counters of other kernel sources (library version %s, commit %s): not reported"
                                 % (prof.get("library_version"), prof.get("git_commit")))
         return (prof["hbm_bytes_per_launch"], prof["valu_busy_frac"],           # the latter from the SQ counters of the same command
-                "profiled offline with rocprofv3 on the same kernel sources, library version %d (%s)" % (version, prof.get("source")))
+                "profiled offline with rocprofv3 on the same kernel sources, library version %s, now %d (%s)"
+                % (prof.get("library_version"), version, prof.get("source")))
     except Exception as e:
         return None, None, "traffic figures unreadable: %r" % (e,)
 
