@@ -339,7 +339,8 @@ typedef enum {
  * With t = min(rne(p 2^rng_bits), 2^rng_bits - 1) it is dropped (becomes 0, whatever it held) iff its draw is below t, and
  * otherwise multiplied by fl32(2^rng_bits / (2^rng_bits - t)), which keeps the mean exactly.  No mask is stored: the backward
  * pass draws the same bits again.  (The other draws of this library have 0, 1 or 2 in the fourth counter word.)
- * A matrix cut between rows gives the same bits as the whole when each part passes its offset, 8 ceil(n/8) times its first row. */
+ * A matrix cut between rows gives the same bits as the whole when each part passes its offset, 8 ceil(n/8) times its first row.  (A
+ * part is a matrix of its own and begins on 16 bytes: where rows are no multiple of 16 bytes, cut where one begins there, or copy.) */
 typedef struct {
     double p;            /* probability of being dropped, 0 <= p < 1                                              */
     uint64_t seed;       /* Philox key                                                                            */

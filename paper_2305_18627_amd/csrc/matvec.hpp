@@ -102,9 +102,10 @@ struct MatvecArgs {
 };
 
 // y = x times the transposed weights: 2 m rows cols operations on rows cols / 2 bytes of codes, which are read once for all rows of x of a
-// slice.  Bound by these bytes for a row or a few (28672x8192, int8, 132 MB with scales: 28-29 us, 4.6 TB/s; a bare read of such codes
-// takes 22); for more rows by what a step costs beside them: x through LDS, unfolding, the barrier (61 rows, 14335x4095: 28.5 us, 250
-// TFLOP/s); for small matrices by latency (4096x4096: 4.2-5 us).
+// slice.  Bound by these bytes for a row or a few (28672x8192, int8, 132 MB with scales: 27.9 us, 4.7 TB/s; a bare read of such codes
+// takes 22); for more rows by what a step costs beside them and does not overlap (61 rows, 14335x4095, fp16, groups of 32: 28.9 us, 248
+// TFLOP/s: vector instructions take 54 % of the cycles, matrix instructions 27 %, LDS 25 %); for small matrices by latency (4096x4096: 4.7
+// us).  These are kernels of a captured graph, one after another; calls from a program overlap at their ends and take up to 3 us less.
 // A workgroup of WN x WK waves owns WN * 16 rows of the weights at a time and up to MT * 16 rows of x; the WK waves share out
 // the columns, 128 U at a time (a step), and their sums are joined in LDS at a tile's end.  x is staged in LDS: RESIDENT, all of
 // it, once, for all tiles of rows that the workgroup takes in turn; otherwise a step's columns at a time into two buffers in
@@ -394,8 +395,8 @@ w4_matvec_kernel(MatvecArgs p)
             for (int i = 0; i < kAhead; i++) store_unit(to, row0 + i * kRowsApart, unit, shift, ahead[i]);
         };
         // Codes are asked for two steps ahead, x one.  No branch is around a load, for what is loaded on one way only is waited for where the
-        // ways join: past the last step its loads come again.  us before and after both: 61 rows of x, 14335x4095, groups of 32, f16 34.3
-        // and 29.8; 64 rows, 8192x8192 29.7, 26.9, 28672x8192 75, 68; 64x14000 33.7, 28.3.  Three sets of codes only as far as 128
+        // ways join: past the last step its loads come again.  us before and after, as measured when this was added: 61 rows of x, 14335x4095, groups of 32,
+        // f16 34.3 and 29.8; 64 rows, 8192x8192 29.7, 26.9; 64x14000 33.7, 28.3.  Three sets of codes only as far as 128
         // registers reach (else they spill: 32 rows, 4096x4096, groups of 32 9.0 and 13.4): 45 words of codes, scales and x, or 56 where the
         // groups' products stay apart and a lane's x is little; and not for 16 rows in int8 (12.6, 13.7).
         constexpr int kWords = 3 * (4 * U + kScaleWords) + kAhead * (int)sizeof(Raw) / 4;
@@ -463,6 +464,8 @@ static gq_status launch_matvec(const MatvecArgs &p, hipStream_t stream)
 //   16384x4096   64: 13.8, 64 (8 waves) 14.7, 32: 19.2  |  64: 17.7, 128 22.6, 32 26.5     |  128 (32) 24.0, 64 (32) 31.2, 128 36.2
 //   18000x4096   64 (8 waves) 19.5, 64 24.8, 32: 26.1   |  128: 22.9, 64 29.5              |  128: 35.7, 128 (32) 42.5, 64 (32) 42.8
 //   28672x8192   64 (8 waves) 38.7, 64 43.6, 32: 58.3   |  128: 46.0, 64 53.3              |  128: 71.7, 128 (32) 82.8, 64 (32) 98.1
+// Groups of 32 under binary32 scales hold most: with 16-bit x the shapes of 2 x 8 and 8 x 2 waves (32 rows of weights, 16 of x; 128, 64) spill 8 to 10 of
+// their 128 registers.
 template <typename X, typename S, int GROUP> static gq_status matvec_of_group(MatvecArgs p, hipStream_t stream)
 {
     const int64_t tiles = (p.rows + 15) / 16;

@@ -81,7 +81,7 @@ struct NormArgs {
 };
 
 // Bound by memory in long launches: 8192x4096 bf16 with a residual and dropout, sum and y written, 45 us, 6.0 TB/s; fp32 without dropout
-// 98 us, 5.5 TB/s.  By latency (the load, the sum's round through the team, the 8-bit maximum's) in short ones: 1x4096 3.2 us.
+// 96 us, 5.6 TB/s.  By latency (the load, the sum's round through the team, the 8-bit maximum's) in short ones: 1x4096 2.2 us, to int8 2.6.
 template <typename T, typename W, int WPR, int STEPS, bool TINY, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads<WPR>)
 rms_norm_kernel(NormArgs p)
