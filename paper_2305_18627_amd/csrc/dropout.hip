@@ -53,17 +53,21 @@ extern "C" gq_status gq_dropout(const void *x, const void *residual, int64_t row
     if (!aligned(x, 16) || !aligned(out, 16) || !aligned_or_null(residual, 16)) return GQ_ERR_INVALID_ARG;
     const bool flat = n >= 8 && (rows == 1 || n % 8 == 0) && flat_fits(rows * (pitch8(n) / 8));      // whole units a row
     if (flat) n *= rows, rows = 1;
-    const int64_t per_row = pitch8(n) / 8, blocks = (rows * per_row + kBlock - 1) / kBlock;
-    if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
-    const Drop d = make_drop(p);
+    const int64_t per_row = pitch8(n) / 8;
+    const Drop whole = make_drop(p);
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         auto go = [&](auto shorter, auto with_residual) {
             constexpr bool SHORT = decltype(shorter)::value, RESIDUAL = decltype(with_residual)::value;
             auto kernel = n < 8 ? dropout_kernel<T, SHORT, RESIDUAL, true, false>
                           : flat ? dropout_kernel<T, SHORT, RESIDUAL, false, true> : dropout_kernel<T, SHORT, RESIDUAL, false, false>;
-            kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)x, (const T *)residual, (T *)out, rows, (uint32_t)per_row, n, d);
-            return launched();
+            return in_launches(rows, per_row, 1, [&](int64_t first, int64_t count) {
+                Drop d = whole;
+                d.first += (uint64_t)first * per_row * 8;
+                kernel<<<(unsigned)((count * per_row + kBlock - 1) / kBlock), kBlock, 0, (hipStream_t)hip_stream>>>(
+                    (const T *)x + first * n, RESIDUAL ? (const T *)residual + first * n : nullptr, (T *)out + first * n, count, (uint32_t)per_row, n, d);
+                return launched();
+            });
         };
         const std::true_type yes;
         const std::false_type no;

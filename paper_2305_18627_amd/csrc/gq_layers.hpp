@@ -129,6 +129,16 @@ template <int UNITS, bool FLAT> __device__ __forceinline__ RowUnit row_unit(uint
     const uint32_t more = at / per_row;
     return {(int64_t)row + more, at - more * per_row};
 }
+// f(first row, rows) for as many rows at a time as one launch covers, `units` units a lane: all of them but for 2^32 units and more
+template <typename F> static inline gq_status in_launches(int64_t rows, int64_t per_row, int units, F &&f)
+{
+    const int64_t most = (0xFFFFFFFFLL / kBlock * kBlock) * units / per_row;
+    for (int64_t first = 0; first < rows; first += most) {
+        const gq_status st = f(first, rows - first < most ? rows - first : most);
+        if (st != GQ_OK) return st;
+    }
+    return GQ_OK;
+}
 static inline bool flat_fits(int64_t units) { return units < 0x7FFFFFFF - 4096; }
 
 // The dropout decision of gq_dropout_params, as the kernels take it.

@@ -162,8 +162,7 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
     // whole groups of units, whole words of codes
     const int64_t row_words = (cols + 31) / 32 * 4, per_row = ((cols + group - 1) / group * group) / 8, units = rows * per_row;
     const bool four = cols >= 8 && dtype != GQ_F32 && units >= kLongQuantize;
-    const int64_t per_block = (four ? 4 : 1) * kBlock, blocks = (units + per_block - 1) / per_block;
-    if (!grid_fits(blocks, kBlock)) return GQ_ERR_INVALID_ARG;
+    const int64_t groups = (cols + group - 1) / group, per_block = (four ? 4 : 1) * kBlock;
     return with_float_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         return with_scale_type(scale_dtype, [&](auto s) {
@@ -177,9 +176,12 @@ gq_status gq_group_quantize(const void *w, int64_t rows, int64_t cols, gq_dtype 
             };
             auto kernel = group == 32 ? of_group(std::integral_constant<int, 32>())
                                       : group == 64 ? of_group(std::integral_constant<int, 64>()) : of_group(std::integral_constant<int, 128>());
-            kernel<<<(unsigned)blocks, kBlock, 0, (hipStream_t)hip_stream>>>((const T *)w, rows, cols, (uint32_t)per_row, (int)((cols + group - 1) / group),
-                                                                           (uint32_t)row_words, (uint32_t *)codes_out, (S *)scales_out);
-            return launched();
+            return in_launches(rows, per_row, four ? 4 : 1, [&](int64_t first, int64_t count) {
+                kernel<<<(unsigned)((count * per_row + per_block - 1) / per_block), kBlock, 0, (hipStream_t)hip_stream>>>(
+                    (const T *)w + first * cols, count, cols, (uint32_t)per_row, (int)groups, (uint32_t)row_words, (uint32_t *)codes_out + first * row_words,
+                    (S *)scales_out + first * groups);
+                return launched();
+            });
         });
     });
 }

@@ -312,3 +312,31 @@ def test_backward_refuses_what_is_no_matrix_like_the_other_calls():
         gq.rms_norm_backward(None, x, w, w, x, dweight_out=w)
     with pytest.raises(ValueError):
         gq.rms_norm_backward(torch.zeros(()), x, w, w, x, dweight_out=w)
+
+
+# ---- as many elements as a call takes ---------------------------------------------------------------------------------
+
+@gpu
+def test_dropout_of_as_many_elements_as_a_matrix_may_have():
+    """2^35 elements, in place: the last rows are those of a call on them alone."""
+    rows, n, last = 1 << 19, 1 << 16, (1 << 19) - 8
+    x = torch.ones(rows, n, dtype=torch.bfloat16, device=DEV)
+    tail = torch.empty(8, n, dtype=x.dtype, device=DEV)
+    gq.dropout(x[last:], gq.make_dropout(0.3, 9, index_base=n * last), tail)
+    middle = torch.empty(8, n, dtype=x.dtype, device=DEV)
+    gq.dropout(x[rows // 2 - 4:rows // 2 + 4], gq.make_dropout(0.3, 9, index_base=n * (rows // 2 - 4)), middle)
+    gq.dropout(x, gq.make_dropout(0.3, 9), x)
+    assert torch.equal(x[last:], tail) and torch.equal(x[rows // 2 - 4:rows // 2 + 4], middle)
+
+
+@gpu
+def test_weights_of_as_many_units_as_a_call_takes():
+    """Short rows of binary32 weights, padded to a group of 128: 2^32 units of eight columns."""
+    rows, cols, last = 1 << 28, 33, (1 << 28) - 8
+    w = torch.empty(rows, cols, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(1))
+    codes = torch.empty(rows, gq.w4_row_bytes(cols), dtype=torch.uint8, device=DEV)
+    scales = torch.empty(rows, 1, device=DEV)
+    gq.group_quantize(w, 128, codes, scales)
+    tc, ts = torch.empty_like(codes[last:]), torch.empty_like(scales[last:])
+    gq.group_quantize(w[last:].clone(), 128, tc, ts)
+    assert torch.equal(codes[last:], tc) and torch.equal(scales[last:], ts)
