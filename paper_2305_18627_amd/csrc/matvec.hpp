@@ -283,9 +283,9 @@ w4_matvec_kernel(MatvecArgs p)
         for (int i = 0; i < MT; i++) *reinterpret_cast<f32x4 *>(part + (wk * WN + wn) * kPerWave + (i * 64 + lane) * 4) = acc[i];
     };
     // Products whose sums are not finite, once more in binary64: the sums of 24 |x| of a bfloat16 row, and 16 times the sum of int8 codes, may
-    // leave binary32 where the product does not.  One after another, the whole wave at each; a row of x that is not finite ends at once, for
-    // all its products.  A column a lane, in few registers, for it is rare: 64 rows of x, 28672x8192, groups of 64, take 20 ms where all
-    // products go this way, 1.3 where each row of x ends in an infinity, 0.08 otherwise.
+    // leave binary32 where the product does not.  One after another, the whole wave at each; a row of x that is not finite ends it for all its
+    // products, a scale of NaN, looked for first, for this one.  A column a lane, in few registers, for it is rare: 64 rows of x,
+    // 28672x8192, groups of 64, take 20 ms where all products go this way, 1.3 where each row of x ends in an infinity, 0.08 otherwise.
     auto once_more = [&](bool wanted, int row_of_x, int row, float &v) {
         for (uint64_t left = __ballot(wanted && !is_finite(v)); left != 0;) {
             const int l = __builtin_ctzll(left), rx = __builtin_amdgcn_readlane(row_of_x, l), rw = __builtin_amdgcn_readlane(row, l);
@@ -295,7 +295,10 @@ w4_matvec_kernel(MatvecArgs p)
             double s = 0.0;
             bool finite = true;
 #pragma unroll 1
-            for (int first = 0; first < p.cols && __all(finite); first += 64) {
+            for (int g = lane; g < p.groups; g += 64)
+                if (const float scale = (float)scales[g]; scale != scale) s = __builtin_nan("");
+#pragma unroll 1
+            for (int first = 0; first < p.cols && __all(finite && s == s); first += 64) {
                 const uint32_t c = (uint32_t)min(first + lane, p.cols - 1);
                 const float f = first + lane < p.cols ? (float)at[c] : 0.0f;
                 finite = is_finite(f);
